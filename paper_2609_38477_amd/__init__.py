@@ -630,3 +630,10 @@ def footprint(clean, corrupt, stream=None):
     c = int(cnt.item())
     s = sums.cpu().numpy()
     return c, c / n, float(np.sqrt(s[0] / s[1])) if s[1] > 0 else float("nan")
+
+
+from .ops import (Q4Weights, TokenLogprobs, q4_dequantize, q4_gemv, q4_quantize,  # noqa: E402,F401
+                  seedq_q4_dequantize, seedq_q4_gemv, seedq_q4_gemv_workspace_bytes,
+                  seedq_q4_quantize, seedq_q4_row_words, seedq_token_logprobs,
+                  seedq_token_logprobs_backward, seedq_token_logprobs_workspace_bytes,
+                  token_logprobs, token_logprobs_backward)
