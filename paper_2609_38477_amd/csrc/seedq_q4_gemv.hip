@@ -1,4 +1,15 @@
 // Products of a 4-bit matrix with vectors, straight from the codes.
+//
+// With u the code and z the zero point (8 without), a row's product with x is
+//     sum over groups g of s_g sum (u - z_g) x = s_g (sum u x - z_g sum x).
+// A byte 0 .. 15 read as an 8-bit float with three mantissa bits stands for u 2^-9 (its
+// subnormals and its first binade), so three operations spread the codes of a word over
+// bytes and four conversions, which also scale, make eight exact 16-bit floats. Their
+// pairs are columns (0, 2), (4, 6), (1, 3), (5, 7); x is put in that order. In fp16 one
+// packed addition takes z off exactly. In bf16, which has none, the kernels form sum u x
+// and take z sum x from it in fp32 once a group. x in fp32 goes to the matrix core as
+// three bf16 pieces of 8 bits (truncated, so that they add up to it exactly) that are
+// multiplied like three vectors: every product is exact and only the fp32 sums round.
 #include <algorithm>
 
 #include "seedq_ops_device.h"
@@ -6,73 +17,449 @@
 namespace seedq {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
 
-// One wave a row, NV vectors at a time: lanes over the row's words, the eight
-// products of a word summed before the scale enters, then a tree over the lanes.
-template <class X, class Y, bool ALIGNED, int NV>
-__global__ void __launch_bounds__(kThreads)
-gemv_kernel(Q4 q, int64_t nvec, const typename X::raw* __restrict__ x, int64_t ldx,
-            typename Y::raw* __restrict__ y, int64_t ldy) {
-  const int lane = int(threadIdx.x & 63);
-  const int64_t r = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  if (r >= q.nrows) return;
-  const uint32_t* codes = q.codes + r * q.row_words;
-  const int64_t words = q.ncols / kC;
-  for (int64_t v0 = int64_t(blockIdx.y) * NV; v0 < nvec; v0 += int64_t(gridDim.y) * NV) {
-    float sum[NV] = {};
-    for (int64_t w = lane; w < words; w += 64) {
-      const uint32_t code = codes[w];
-      const int64_t g = r * q.ngroups + ((w * 8) >> q.gshift);
-      const float s = F16::widen(q.scale[g]);
-      const float z = q.zero ? float(q.zero[g] & 15) : 8.f;
-      float u[8];
+constexpr float kCodeScale = 512.f;   // 2^9
+
+// The 16-bit arithmetic of a kernel. kCentred: codes have their zero point taken off.
+struct Half {
+  static constexpr bool kCentred = true;
+  static constexpr uint32_t kOnes = 0x3C003C00u;
+  template <bool HIGH>
+  __device__ static __forceinline__ f16x2 pair(uint32_t bytes) {
+    return __builtin_bit_cast(
+        f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(bytes, kCodeScale, HIGH));
+  }
+  __device__ static __forceinline__ floatx4 mfma(uint32x4 a, uint32x4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+struct Brain {
+  static constexpr bool kCentred = false;
+  static constexpr uint32_t kOnes = 0x3F803F80u;
+  template <bool HIGH>
+  __device__ static __forceinline__ bf16x2 pair(uint32_t bytes) {
+    return __builtin_bit_cast(
+        bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, kCodeScale, HIGH));
+  }
+  __device__ static __forceinline__ floatx4 mfma(uint32x4 a, uint32x4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+
+// The eight codes of a word as 16-bit floats in code order.
+template <class M>
+__device__ __forceinline__ uint32x4 decode(uint32_t w) {
+  const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+  return uint32x4{__builtin_bit_cast(uint32_t, M::template pair<false>(even)),
+                  __builtin_bit_cast(uint32_t, M::template pair<true>(even)),
+                  __builtin_bit_cast(uint32_t, M::template pair<false>(odd)),
+                  __builtin_bit_cast(uint32_t, M::template pair<true>(odd))};
+}
+__device__ __forceinline__ uint32x4 centred(uint32x4 u, f16x2 z) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = float((code >> (4 * i)) & 15u) - z;
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t pair = u[j];   // a bit cast of a vector's element takes element 0
+    u[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - z);
+  }
+  return u;
+}
+
+// Column of element i of the code order.
+constexpr int kOrder[8] = {0, 2, 4, 6, 1, 3, 5, 7};
+// Eight consecutive 16-bit elements into code order.
+__device__ __forceinline__ uint32x4 to_code_order(uint32x4 d) {
+  return uint32x4{__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
+                  __builtin_amdgcn_perm(d[3], d[2], 0x05040100u),
+                  __builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
+                  __builtin_amdgcn_perm(d[3], d[2], 0x07060302u)};
+}
+
+// Eight 16-bit elements as they lie; `aligned` to 16 bytes is the same for all lanes.
+__device__ __forceinline__ uint32x4 load8_raw(const uint16_t* p, bool aligned) {
+  if (aligned) return *reinterpret_cast<const uint32x4*>(p);
+  uint32x4 d;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float f[8];
-        const int64_t vv = std::min(v0 + v, nvec - 1);
-        load8<X, ALIGNED>(x + vv * ldx + w * 8, f);
-        float t = u[0] * f[0];
+  for (int i = 0; i < 4; ++i) d[i] = uint32_t(p[2 * i]) | uint32_t(p[2 * i + 1]) << 16;
+  return d;
+}
+
+// Eight fp32 values as three bf16 pieces in code order.
+__device__ __forceinline__ void split8(const float (&f)[8], uint32x4 (&piece)[3]) {
+  uint32_t h[3][8];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) t = fmaf(u[i], f[i], t);
-        sum[v] = fmaf(s, t, sum[v]);
+  for (int i = 0; i < 8; ++i) {
+    float r = f[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      h[p][i] = __builtin_bit_cast(uint32_t, r);
+      r -= __builtin_bit_cast(float, h[p][i] & 0xFFFF0000u);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      piece[p][j] = __builtin_amdgcn_perm(h[p][kOrder[2 * j + 1]], h[p][kOrder[2 * j]], 0x07060302u);
+}
+
+__device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v) {
+  if (ytype == SEEDQ_F32) static_cast<float*>(y)[at] = v;
+  else static_cast<uint16_t*>(y)[at] = ytype == SEEDQ_F16 ? F16::narrow(v) : BF16::narrow(v);
+}
+
+// ---------------------------------------------------------------- few vectors
+
+// One or two vectors, on the vector ALU. A wave holds a slab of columns of x in
+// registers, WORDS words of codes a lane, and goes over kRows rows whose codes it reads
+// at once; a lane's columns lie in one group, so the scale enters once a lane and row.
+// The products u - z (fp16) times x (widened to fp32) are fused multiply-adds that read
+// either half of a register. Order of the sums: the columns of a lane, the slabs of a
+// wave, the lanes as a tree, the waves one after the other.
+constexpr int kRows = 8;
+constexpr int kMaxWaves = 16;
+
+template <class X, int NV, int WORDS>
+__global__ void __launch_bounds__(64 * kMaxWaves)
+gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, bool aligned, int slabs,
+                void* __restrict__ y, int ytype, int64_t ldy) {
+  __shared__ float part[kMaxWaves][NV][kRows];
+  const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), waves = int(blockDim.x >> 6);
+  const int64_t r0 = int64_t(blockIdx.x) * kRows;
+  float acc[NV][kRows] = {};
+  for (int slab = wave; slab < slabs; slab += waves) {
+    const int64_t w0 = (int64_t(slab) * 64 + lane) * WORDS;
+    const int64_t wl = w0 * kC < q.ncols ? w0 : 0;   // idle lanes: the row's start, x as zeros
+    const int64_t g = wl * kC >> q.gshift;
+    uint32_t code[kRows][WORDS];
+    float s[kRows], z[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int64_t r = std::min(r0 + i, q.nrows - 1);
+      const uint32_t* p = q.codes + r * q.row_words + wl;
+      if constexpr (WORDS == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        code[i][0] = v.x, code[i][1] = v.y, code[i][2] = v.z, code[i][3] = v.w;
+      } else if constexpr (WORDS == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        code[i][0] = v.x, code[i][1] = v.y;
+      } else {
+        code[i][0] = *p;
+      }
+      s[i] = F16::widen(q.scale[r * q.ngroups + g]);
+      z[i] = q.zero ? float(q.zero[r * q.ngroups + g] & 15) : 8.f;
+    }
+    float xf[NV][WORDS][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        const int64_t c = (w0 + w) * kC;
+        const typename X::raw* xv = x + v * ldx + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xf[v][w][i] = 0.f;
+        if (c < q.ncols) aligned ? load8<X, true>(xv, xf[v][w]) : load8<X, false>(xv, xf[v][w]);
+      }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      float d[NV] = {};
+      const f16x2 zz = {_Float16(z[i]), _Float16(z[i])};
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        const uint32x4 u = centred(decode<Half>(code[i][w]), zz);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t bits = u[j];
+          const f16x2 pair = __builtin_bit_cast(f16x2, bits);
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            d[v] = fmaf(float(pair[0]), xf[v][w][kOrder[2 * j]], d[v]);
+            d[v] = fmaf(float(pair[1]), xf[v][w][kOrder[2 * j + 1]], d[v]);
+          }
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) acc[v][i] = fmaf(s[i], d[v], acc[v][i]);
+    }
+  }
+  // the eight rows' sums over the lanes: halves of the rows change sides with halves of
+  // the lanes, so that lane l ends with row l / 8
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+#pragma unroll
+    for (int n = kRows / 2, d = 32; n >= 1; n >>= 1, d >>= 1) {
+      const bool up = (lane & d) != 0;
+#pragma unroll
+      for (int k = 0; k < n; ++k) {
+        const float keep = up ? acc[v][k + n] : acc[v][k], give = up ? acc[v][k] : acc[v][k + n];
+        acc[v][k] = keep + __shfl_xor(give, d, 64);
+      }
+    }
+    float t = acc[v][0];
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) t += __shfl_xor(t, d, 64);
+    if ((lane & 7) == 0) part[wave][v][lane >> 3] = t;
+  }
+  __syncthreads();
+  for (int k = int(threadIdx.x); k < NV * kRows; k += int(blockDim.x)) {
+    const int v = k / kRows, i = k % kRows;
+    float t = part[0][v][i];
+    for (int w = 1; w < waves; ++w) t += part[w][v][i];
+    if (r0 + i < q.nrows) store_y(y, ytype, v * ldy + r0 + i, t);
+  }
+}
+
+// ---------------------------------------------------------------- a batch of vectors
+
+// x in fp32 as three bf16 rows a vector (row 3 v + p), in code order, zeros from ncols
+// to the padded end of the codes' rows.
+__global__ void __launch_bounds__(256)
+split_kernel(const float* __restrict__ x, int64_t ldx, bool aligned, int64_t ncols, int64_t row_words,
+             uint16_t* __restrict__ out) {
+  const int64_t v = blockIdx.y;
+  const int64_t w = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (w >= row_words) return;
+  float f[8] = {};
+  if (w * kC < ncols) {
+    const float* p = x + v * ldx + w * kC;
+    aligned ? load8<F32, true>(p, f) : load8<F32, false>(p, f);
+  }
+  uint32x4 piece[3];
+  split8(f, piece);
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    *reinterpret_cast<uint32x4*>(out + ((3 * v + p) * row_words + w) * kC) = piece[p];
+}
+
+// Up to 16 MT rows of x (vectors, or a third of a vector in fp32) on the matrix core,
+// D = X W^T: a 16x16x32 product takes 16 rows of x and 16 rows of codes. A lane
+// reads 16 bytes of codes of row l % 16, columns 32 (l / 16) .. of a chunk of 128. Where
+// a group is 128 columns or more, product t takes everybody's word t; in smaller groups
+// (NG = 4 or 2 a chunk) the words first change lanes so that product t holds columns
+// 32 t .. 32 t + 31 (four lane swaps). Each group's product and, in bf16, sum of x (a
+// product with ones) meet in fp32 with the scale and zero point of the lane's row. The waves of
+// a workgroup take its chunks in turn and add their sums through LDS in order.
+template <class M, int NG, int RT, int MT>
+struct Chunk {
+  uint32x4 code[RT];
+  float s[RT][NG], z[RT][NG];
+  uint32x4 x[MT][4];
+};
+
+template <class M, int P, int NG, int RT, int MT>
+__global__ void __launch_bounds__(64 * kMaxWaves / (MT == 4 ? 2 : 1))
+gemv_batch_kernel(Q4 q, int64_t nvec, const uint16_t* __restrict__ x, int64_t ldx, bool aligned,
+                  void* __restrict__ y, int ytype, int64_t ldy) {
+  constexpr int kVec = 16 * MT / P;   // vectors of a workgroup
+  extern __shared__ float part[];
+  const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), waves = int(blockDim.x >> 6);
+  const int n = lane & 15, kg = lane >> 4;
+  const int64_t v0 = int64_t(blockIdx.y) * kVec;
+  const int nv = int(std::min<int64_t>(kVec, nvec - v0));
+  const int64_t r0 = int64_t(blockIdx.x) * (16 * RT);
+  const int64_t xcols = P == 3 ? q.row_words * kC : q.ncols;
+  const int64_t chunks = (q.ncols + 127) / 128;
+  const uint16_t* xrow[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)   // rows past the last are read as the last and not stored
+    xrow[m] = x + (v0 * P + std::min(16 * m + n, nv * P - 1)) * ldx;
+  const uint32_t* crow[RT];
+  int64_t grow[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int64_t r = std::min(r0 + 16 * t + n, q.nrows - 1);
+    crow[t] = q.codes + r * q.row_words;
+    grow[t] = r * q.ngroups;
+  }
+  auto load = [&](Chunk<M, NG, RT, MT>& c, int64_t ch) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int64_t w = ch * 16 + kg * 4;
+      c.code[t] = uint32x4{0u, 0u, 0u, 0u};
+      if (w < q.row_words) c.code[t] = *reinterpret_cast<const uint32x4*>(crow[t] + w);
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        const int64_t g = grow[t] + std::min((ch * 128 + j * (128 / NG)) >> q.gshift, q.ngroups - 1);
+        c.s[t][j] = F16::widen(q.scale[g]);
+        c.z[t][j] = q.zero ? float(q.zero[g] & 15) : 8.f;
       }
     }
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) sum[v] += __shfl_xor(sum[v], d, 64);
-      if (lane == 0 && v0 + v < nvec) y[(v0 + v) * ldy + r] = Y::narrow(sum[v]);
+      for (int t = 0; t < 4; ++t) {
+        const int64_t k = ch * 128 + (NG == 1 ? kg * 32 + t * 8 : t * 32 + kg * 8);
+        c.x[m][t] = uint32x4{0u, 0u, 0u, 0u};
+        if (k < xcols) c.x[m][t] = load8_raw(xrow[m] + k, aligned);
+      }
+  };
+  floatx4 sum[RT][MT] = {};
+  Chunk<M, NG, RT, MT> c;
+  if (wave < chunks) load(c, wave);
+  for (int64_t ch = wave; ch < chunks; ch += waves) {
+    Chunk<M, NG, RT, MT> next = c;
+    if (ch + waves < chunks) load(next, ch + waves);
+    if constexpr (P == 1)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) c.x[m][t] = to_code_order(c.x[m][t]);
+    const uint32x4 ones = {M::kOnes, M::kOnes, M::kOnes, M::kOnes};
+    floatx4 xs[MT][NG] = {};
+    if constexpr (!M::kCentred)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) xs[m][t * NG / 4] = M::mfma(c.x[m][t], ones, xs[m][t * NG / 4]);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      uint32x4 w = c.code[t];
+      if constexpr (NG > 1) {
+        const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        const auto e = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+        const auto f = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+        w = uint32x4{e[0], e[1], f[0], f[1]};
+      }
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        floatx4 acc[MT] = {};
+#pragma unroll
+        for (int k = j * 4 / NG; k < (j + 1) * 4 / NG; ++k) {
+          uint32x4 u = decode<M>(w[k]);
+          if constexpr (M::kCentred) u = centred(u, f16x2{_Float16(c.z[t][j]), _Float16(c.z[t][j])});
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[m] = M::mfma(c.x[m][k], u, acc[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sum[t][m][i] = fmaf(
+                c.s[t][j], M::kCentred ? acc[m][i] : fmaf(-c.z[t][j], xs[m][j][i], acc[m][i]),
+                sum[t][m][i]);
+      }
     }
+    c = next;
   }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        part[(((wave * RT + t) * MT + m) * 4 + i) * 64 + lane] = sum[t][m][i];
+  __syncthreads();
+  // row 4 kg + i of x and row n of the codes lie in lane 16 kg + n, register i
+  for (int k = int(threadIdx.x); k < nv * RT * 16; k += int(blockDim.x)) {
+    const int rn = k % (16 * RT), v = k / (16 * RT);
+    const int64_t r = r0 + rn;
+    float total = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int row = P * v + p, m = row >> 4;
+      const int at = (((rn >> 4) * MT + m) * 4 + (row & 3)) * 64 + ((row >> 2) & 3) * 16 + (rn & 15);
+      float one = part[at];
+      for (int w = 1; w < waves; ++w) one += part[w * (RT * MT * 256) + at];
+      total += one;
+    }
+    if (r < q.nrows) store_y(y, ytype, (v0 + v) * ldy + r, total);
+  }
+}
+
+bool few(int64_t nvec) { return nvec <= 2; }
+
+template <class X>
+hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, void* d_y, int ytype,
+                      int64_t ldy, hipStream_t stream) {
+  using raw = typename X::raw;
+  const int64_t words = (q.ncols + kC - 1) / kC;
+  const bool al = rows_aligned(d_x, ldx, sizeof(raw));
+  const unsigned grid = unsigned((q.nrows + kRows - 1) / kRows);
+  const int per = words > 128 ? 4 : words > 64 ? 2 : 1;
+  const int slabs = int((words + 64 * per - 1) / (64 * per));
+  const int waves = std::min(slabs, kMaxWaves);
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), 0, stream, q, static_cast<const raw*>(d_x),
+                       ldx, al, slabs, d_y, ytype, ldy);
+    return hipGetLastError();
+  };
+  auto words_of = [&](auto nv) {
+    constexpr int NV = decltype(nv)::value;
+    return per == 4   ? go(gemv_few_kernel<X, NV, 4>)
+           : per == 2 ? go(gemv_few_kernel<X, NV, 2>)
+                      : go(gemv_few_kernel<X, NV, 1>);
+  };
+  return nvec == 1 ? words_of(std::integral_constant<int, 1>{})
+                   : words_of(std::integral_constant<int, 2>{});
+}
+
+template <class M, int P>
+hipError_t launch_batch(const Q4& q, int64_t nvec, const uint16_t* x, int64_t ldx, bool aligned,
+                        void* d_y, int ytype, int64_t ldy, hipStream_t stream) {
+  const int64_t rows = nvec * P, chunks = (q.ncols + 127) / 128;
+  auto go = [&](auto ng, auto rt, auto mt) {
+    constexpr int NG = decltype(ng)::value, RT = decltype(rt)::value, MT = decltype(mt)::value;
+    constexpr int kVec = 16 * MT / P;
+    const int waves = int(std::min<int64_t>(MT == 4 ? 8 : 16, chunks));
+    for (int64_t v = 0; v < nvec; v += 65535 * kVec) {   // the grid's second dimension has 16 bits
+      const int64_t n = std::min<int64_t>(65535 * kVec, nvec - v);
+      const dim3 grid(unsigned((q.nrows + 16 * RT - 1) / (16 * RT)), unsigned((n + kVec - 1) / kVec));
+      hipLaunchKernelGGL((gemv_batch_kernel<M, P, NG, RT, MT>), grid, dim3(64 * waves),
+                         size_t(waves) * RT * MT * 1024, stream, q, n, x + v * P * ldx, ldx, aligned,
+                         static_cast<char*>(d_y) + v * ldy * (ytype == SEEDQ_F32 ? 4 : 2), ytype, ldy);
+    }
+    return hipGetLastError();
+  };
+  auto with_mt = [&](auto ng, auto rt) {
+    return rows <= 16   ? go(ng, rt, std::integral_constant<int, 1>{})
+           : rows <= 32 ? go(ng, rt, std::integral_constant<int, 2>{})
+                        : go(ng, rt, std::integral_constant<int, 4>{});
+  };
+  auto with_rt = [&](auto ng) {
+    return q.nrows >= 32 * 256 ? with_mt(ng, std::integral_constant<int, 2>{})
+                               : with_mt(ng, std::integral_constant<int, 1>{});
+  };
+  return q.gshift >= 7   ? with_rt(std::integral_constant<int, 1>{})
+         : q.gshift == 6 ? with_rt(std::integral_constant<int, 2>{})
+                         : with_rt(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
 
-size_t q4_gemv_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t q4_gemv_workspace_bytes(int64_t, int64_t ncols, int64_t nvec, int xtype) {
+  if (xtype != SEEDQ_F32 || few(nvec)) return 0;
+  return align256(size_t(nvec) * 3 * q4_row_words(ncols) * kC * sizeof(uint16_t));
+}
 
 hipError_t launch_q4_gemv(const Q4& q, int64_t nvec, const void* d_x, int xtype, int64_t ldx,
-                          void* d_y, int ytype, int64_t ldy, void*, hipStream_t stream) {
-  return with_type(xtype, [&](auto tx) {
-    using X = decltype(tx);
-    auto launch = [&](auto ty) {
-      using Y = decltype(ty);
-      const dim3 grid(unsigned((q.nrows + kWaves - 1) / kWaves),
-                      unsigned(std::min<int64_t>((nvec + 3) / 4, 65535)));
-      auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, stream, q, nvec,
-                           static_cast<const typename X::raw*>(d_x), ldx,
-                           static_cast<typename Y::raw*>(d_y), ldy);
-      };
-      rows_aligned(d_x, ldx, sizeof(typename X::raw)) ? go(gemv_kernel<X, Y, true, 4>)
-                                                      : go(gemv_kernel<X, Y, false, 4>);
-      return hipGetLastError();
-    };
-    return ytype == SEEDQ_F32 ? launch(F32{}) : launch(tx);
-  });
+                          void* d_y, int ytype, int64_t ldy, void* d_ws, hipStream_t stream) {
+  if (few(nvec))
+    return with_type(xtype, [&](auto t) {
+      return launch_few<decltype(t)>(q, nvec, d_x, ldx, d_y, ytype, ldy, stream);
+    });
+  if (xtype == SEEDQ_F32) {
+    uint16_t* pieces = static_cast<uint16_t*>(d_ws);
+    const bool al = rows_aligned(d_x, ldx, 4);
+    for (int64_t v = 0; v < nvec; v += 65535) {   // the grid's second dimension has 16 bits
+      const int64_t n = std::min<int64_t>(65535, nvec - v);
+      hipLaunchKernelGGL(split_kernel, dim3(unsigned((q.row_words + 255) / 256), unsigned(n)),
+                         dim3(256), 0, stream, static_cast<const float*>(d_x) + v * ldx, ldx, al,
+                         q.ncols, q.row_words, pieces + v * 3 * q.row_words * kC);
+    }
+    return launch_batch<Brain, 3>(q, nvec, pieces, q.row_words * kC, true, d_y, ytype, ldy, stream);
+  }
+  const bool al = rows_aligned(d_x, ldx, 2);
+  const uint16_t* x = static_cast<const uint16_t*>(d_x);
+  return xtype == SEEDQ_F16 ? launch_batch<Half, 1>(q, nvec, x, ldx, al, d_y, ytype, ldy, stream)
+                            : launch_batch<Brain, 1>(q, nvec, x, ldx, al, d_y, ytype, ldy, stream);
 }
 
 }  // namespace seedq
