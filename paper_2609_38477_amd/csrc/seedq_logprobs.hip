@@ -1,142 +1,509 @@
 // Log probabilities of given tokens with entropy and top alternatives, and their
 // gradient at the logits.
+//
+// Both are one pass over the logits in 16-byte vectors, bound by memory. Forward, each
+// thread keeps a running maximum m and, relative to it, S = sum e^(x - m) and
+// E = sum e^(x - m) (x - m); a larger maximum rescales both. The threads' sums meet in
+// fp64. The entropy log S - E / S adds two terms of one sign.
 #include <algorithm>
+#include <cfloat>
 
 #include "seedq_ops_device.h"
 
 namespace seedq {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr float kInf = __builtin_inff();
+typedef unsigned long long Key;
 
-template <class V, class F>
-__device__ V block_reduce(V v, V* shared, F f) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = f(v, __shfl_xor(v, d, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = shared[0];
-  for (int w = 1; w < int(blockDim.x >> 6); ++w) v = f(v, shared[w]);
-  return v;
-}
+constexpr float kInf = __builtin_inff();
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kFar = -1e30f;      // stands in for x - m = -inf: its e^ is 0, and so is 0 x kFar
+constexpr int kUnroll = 4;          // vectors in flight a thread
+constexpr int kMaxTop = SEEDQ_MAX_TOP;
+constexpr int kPicked = 512;        // threads that may hold an alternative: kMaxTop groups of 16
+constexpr int kFound = 1024;        // elements collected before the slow selection steps in
+constexpr int kMaxSegs = 32;
 
 // Order of alternatives in one number: the value's pattern made monotonic (-0 is
-// 0), then the lower token first. 0 stands for none.
-__device__ __forceinline__ unsigned long long order_key(float x, uint32_t v) {
+// 0), then the lower index first. 0 stands for none.
+__device__ __forceinline__ Key order_key(float x, uint32_t index) {
   const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
   const uint32_t k = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return (static_cast<unsigned long long>(k) << 32) | (0xFFFFFFFFu - v);
+  return (Key(k) << 32) | (0xFFFFFFFFu - index);
 }
-__device__ __forceinline__ float key_value(unsigned long long key) {
+__device__ __forceinline__ float key_value(Key key) {
   const uint32_t k = uint32_t(key >> 32);
   return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
-__device__ __forceinline__ uint32_t key_token(unsigned long long key) {
-  return 0xFFFFFFFFu - uint32_t(key);
-}
+__device__ __forceinline__ uint32_t key_index(Key key) { return 0xFFFFFFFFu - uint32_t(key); }
+__device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 
-// One workgroup a row: the maximum, the sums, then one pass for each alternative.
+// A row in 16-byte vectors: `head` elements before the first boundary, then vectors,
+// then the rest.
 template <class T>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(LogprobArgs a) {
-  __shared__ double sd[kWaves];
-  __shared__ float sf[kWaves];
-  __shared__ unsigned long long sk[kWaves];
-  const int64_t t = blockIdx.x;
-  const typename T::raw* x = static_cast<const typename T::raw*>(a.logits) + t * a.ld;
-  const int64_t V = a.vocab;
-  float m = -kInf, bad = 0.f;
-  for (int64_t v = threadIdx.x; v < V; v += kThreads) {
-    const float f = T::widen(x[v]);
-    m = fmaxf(m, f);
-    if (!(f < kInf)) bad = 1.f;
+struct Row {
+  static constexpr int N = 16 / sizeof(typename T::raw);
+  const typename T::raw* x;
+  int64_t vectors;
+  int head, tail;
+  __device__ Row(const typename T::raw* p, int64_t n) : x(p) {
+    const int64_t h = int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(*p);
+    head = int(std::min<int64_t>(h, n));
+    vectors = (n - head) / N;
+    tail = int(n - head - vectors * N);
   }
-  m = block_reduce(m, sf, [](float p, float q) { return fmaxf(p, q); });
-  bad = block_reduce(bad, sf, [](float p, float q) { return fmaxf(p, q); });
-  double S = 0, E = 0;
-  if (m > -kInf) {
-    for (int64_t v = threadIdx.x; v < V; v += kThreads) {
-      const float d = T::widen(x[v]) - m;
-      const float e = expf(d);
-      S += e;
-      if (e > 0.f) E += double(e) * d;
-    }
+  __device__ __forceinline__ uint4 load(int64_t i) const {
+    return *reinterpret_cast<const uint4*>(x + head + i * N);
   }
-  S = block_reduce(S, sd, [](double p, double q) { return p + q; });
-  E = block_reduce(E, sd, [](double p, double q) { return p + q; });
-  const bool empty = !(m > -kInf);
-  const double logS = bad ? double(__builtin_nanf("")) : empty ? 0.0 : log(S);
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[t] = float(double(m) + logS);
-    if (a.entropy) a.entropy[t] = bad ? __builtin_nanf("") : empty ? 0.f : float(logS - E / S);
-    if (a.logprob) {
-      const int64_t tok = a.tokens[t];
-      float lp = 0.f;
-      if (tok >= V) lp = __builtin_nanf("");
-      else if (tok >= 0) lp = empty && !bad ? -kInf : float(double(T::widen(x[tok])) - m - logS);
-      a.logprob[t] = lp;
-    }
-  }
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    unsigned long long best = 0;
-    if (!bad && last)
-      for (int64_t v = threadIdx.x; v < V; v += kThreads) {
-        const float f = T::widen(x[v]);
-        const unsigned long long key = order_key(f, uint32_t(v));
-        if (f > -kInf && key < last && key > best) best = key;
+  __device__ static __forceinline__ void widen(uint4 v, float (&f)[N]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (N == 4) {
+        f[i] = __builtin_bit_cast(float, w[i]);
+      } else {
+        f[2 * i] = T::widen(uint16_t(w[i] & 0xFFFFu));
+        f[2 * i + 1] = T::widen(uint16_t(w[i] >> 16));
       }
-    best = block_reduce(best, sk, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
-    if (threadIdx.x == 0) {
-      a.top_token[t * a.top + k] = best ? int64_t(key_token(best)) : -1;
-      a.top_logprob[t * a.top + k] =
-          bad ? __builtin_nanf("") : best ? float(double(key_value(best)) - m - logS) : -kInf;
     }
-    last = best;
+  }
+};
+
+struct Sums {
+  float m = -FLT_MAX, S = 0.f, E = 0.f;
+  float best = -kInf;       // the largest element seen and the first vector that has it
+  uint32_t base = 0;
+
+  __device__ __forceinline__ void raise(float to) {
+    if (to > m) {
+      const float d = fmaxf(m - to, kFar);
+      const float c = __builtin_amdgcn_exp2f(d * kLog2E);
+      E = c * fmaf(d, S, E);
+      S *= c;
+      m = to;
+    }
+  }
+  __device__ __forceinline__ void add(float x) {
+    // a NaN stays one: m is infinite only in a row without a distribution
+    const float d = __builtin_elementwise_maximum(x - m, kFar);
+    const float e = __builtin_amdgcn_exp2f(d * kLog2E);
+    S += e;
+    E = fmaf(e, d, E);
+  }
+  __device__ __forceinline__ void note(float largest, uint32_t at) {
+    if (largest > best) {
+      best = largest;
+      base = at;
+    }
+  }
+};
+
+template <int N>
+__device__ __forceinline__ float largest(const float (&f)[N]) {
+  float t = f[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) t = fmaxf(t, f[i]);
+  return t;
+}
+
+// What a segment of a row hands to the join.
+struct Partial {
+  double S, E;
+  float m, unused;
+};
+
+// The outputs of row t but for the alternatives, by one thread.
+template <class T>
+__device__ void write_sums(const LogprobArgs& a, int64_t t, float m, double S, double E, double& log_s) {
+  const double nan = __builtin_nan("");
+  const bool empty = S == 0.0;
+  log_s = empty ? -double(kInf) : log(S);   // NaN where S is
+  if (a.lse) a.lse[t] = empty ? -kInf : float(double(m) + log_s);
+  if (a.entropy) a.entropy[t] = empty ? 0.f : float(log_s - E / S);
+  if (a.logprob) {
+    const int64_t tok = a.tokens[t];
+    double lp = 0.0;
+    if (tok >= a.vocab) lp = nan;
+    else if (tok >= 0) {
+      const float x = T::widen(static_cast<const typename T::raw*>(a.logits)[t * a.ld + tok]);
+      lp = empty ? -double(kInf) : (double(x) - m) - log_s;
+    }
+    a.logprob[t] = float(lp);
   }
 }
 
+__device__ __forceinline__ void write_alternative(const LogprobArgs& a, int64_t t, int k, Key key,
+                                                  float m, double log_s) {
+  const bool bad = !(log_s <= double(FLT_MAX));   // NaN
+  const bool none = bad || key == 0;
+  a.top_token[t * a.top + k] = none ? -1 : int64_t(key_index(key));
+  a.top_logprob[t * a.top + k] =
+      bad ? __builtin_nanf("") : none ? -kInf : float((double(key_value(key)) - m) - log_s);
+}
+
+// The keys of list[0 .. n) in falling order: f(rank, key) for the first `top` ranks.
+template <class F>
+__device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
+  for (int i = int(threadIdx.x); i < n; i += int(blockDim.x)) {
+    const Key mine = list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
+    if (rank < top) f(rank, mine);
+  }
+}
+
+// One workgroup of NT threads a row, or a segment of one (blockIdx.y of segs), whose
+// sums and alternatives then go to the join.
+//
+// Alternatives: each thread remembers its largest element and the vector that first had
+// it. The top-th largest of these over the threads (found in two steps, over 64 groups of
+// threads and over the threads of the groups that reach it) bounds the top-th largest
+// element from below, so only vectors of the at most kMaxTop threads that reach the
+// bound are read again, each thread's by its whole wave, and the elements that reach it
+// are ranked against each other. Vectors are intervals of the row, so the order of
+// (value, first vector) is that of (value, index), and ties are cut the same way.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
+                                                      Partial* __restrict__ partial,
+                                                      Key* __restrict__ seg_top) {
+  constexpr int N = Row<T>::N, kWaves = NT / 64, kGroup = NT / 64;
+  __shared__ double sd[2][kWaves];
+  __shared__ float sf[kWaves];
+  __shared__ Key group_key[64], picked[kPicked], found[kFound], cut;
+  __shared__ int npicked, nfound;
+  const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.x;
+  const int seg = int(blockIdx.y);
+  const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
+  const int64_t begin = row.vectors * seg / segs, end = row.vectors * (seg + 1) / segs;
+  Sums s;
+  auto one = [&](int64_t i) {
+    const float x = T::widen(row.x[i]);
+    s.raise(x);
+    s.add(x);
+    s.note(x, uint32_t(i));
+  };
+  if (seg == 0 && tid < row.head) one(tid);
+  int64_t i = begin + tid;
+  for (; i + (kUnroll - 1) * NT < end; i += kUnroll * NT) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = row.load(i + u * NT);
+    float f[kUnroll][N], top = -kInf;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      Row<T>::widen(v[u], f[u]);
+      const float l = largest(f[u]);
+      s.note(l, uint32_t(row.head + (i + u * NT) * N));
+      top = fmaxf(top, l);
+    }
+    s.raise(top);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int k = 0; k < N; ++k) s.add(f[u][k]);
+  }
+  for (; i < end; i += NT) {
+    float f[N];
+    Row<T>::widen(row.load(i), f);
+    const float l = largest(f);
+    s.note(l, uint32_t(row.head + i * N));
+    s.raise(l);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s.add(f[k]);
+  }
+  if (seg == segs - 1 && tid < row.tail) one(a.vocab - row.tail + tid);
+
+  // the sums of the threads
+  float m = s.m;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  if (lane == 0) sf[wave] = m;
+  if (tid == 0) {
+    npicked = nfound = 0;
+    cut = 1;
+  }
+  __syncthreads();
+  m = sf[0];
+  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sf[w]);
+  const float d = fmaxf(s.m - m, kFar);
+  const double c = __builtin_amdgcn_exp2f(d * kLog2E);
+  double S = c * s.S, E = c * (s.E + double(d) * s.S);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    S += __shfl_xor(S, k, 64);
+    E += __shfl_xor(E, k, 64);
+  }
+  if (lane == 0) {
+    sd[0][wave] = S;
+    sd[1][wave] = E;
+  }
+  // the largest element of each of 64 groups of threads
+  const Key mine = s.best > -kInf ? order_key(s.best, s.base) : 0;
+  Key g = mine;
+#pragma unroll
+  for (int k = 1; k < kGroup; k <<= 1) g = max_key(g, __shfl_xor(g, k, 64));
+  if (tid % kGroup == 0) group_key[tid / kGroup] = g;
+  __syncthreads();
+  S = sd[0][0], E = sd[1][0];
+  for (int w = 1; w < kWaves; ++w) {
+    S += sd[0][w];
+    E += sd[1][w];
+  }
+  double log_s = 0.0;
+  const int64_t part = t * segs + seg;
+  if (segs > 1) {
+    if (tid == 0) partial[part] = Partial{S, E, m, 0.f};
+  } else {
+    if (tid == 0) write_sums<T>(a, t, m, S, E, log_s);
+    else if (a.top) log_s = S == 0.0 ? -double(kInf) : log(S);
+  }
+  if (a.top == 0) return;
+  auto put = [&](int rank, Key key) {
+    if (segs > 1) seg_top[part * a.top + rank] = key;
+    else write_alternative(a, t, rank, key, m, log_s);
+  };
+  if (!(S > 0.0)) {   // nothing left, or no distribution (the same for all threads)
+    for (int k = tid; k < a.top; k += NT) put(k, 0);
+    return;
+  }
+  {   // bound over the groups: every wave for itself
+    const Key key = group_key[lane];
+    int rank = 0;
+    for (int j = 0; j < 64; ++j) rank += group_key[j] > key ? 1 : 0;
+    const unsigned long long at = __ballot(rank == a.top - 1);
+    const Key bound = at ? __shfl(key, __builtin_ctzll(at), 64) : 0;
+    if (mine && mine >= bound) picked[atomicAdd(&npicked, 1)] = mine;
+  }
+  __syncthreads();
+  by_rank(picked, npicked, a.top, [&](int rank, Key key) {
+    if (rank == a.top - 1) cut = key;
+  });
+  __syncthreads();
+  const Key bound = cut;
+  auto take = [&](float x, int64_t index, int64_t base) {
+    if (x > -kInf && order_key(x, uint32_t(base)) >= bound) {
+      const int k = atomicAdd(&nfound, 1);
+      if (k < kFound) found[k] = order_key(x, uint32_t(index));
+    }
+  };
+  if (mine >= bound) {   // its single elements
+    if (seg == 0 && tid < row.head) take(T::widen(row.x[tid]), tid, tid);
+    const int64_t last = a.vocab - row.tail + tid;
+    if (seg == segs - 1 && tid < row.tail) take(T::widen(row.x[last]), last, last);
+  }
+  for (unsigned long long todo = __ballot(mine >= bound); todo; todo &= todo - 1) {
+    const int64_t first = begin + wave * 64 + __builtin_ctzll(todo);
+    for (int64_t v = first + int64_t(lane) * NT; v < end; v += int64_t(64) * NT) {
+      float f[N];
+      Row<T>::widen(row.load(v), f);
+      const int64_t base = row.head + v * N;
+      if (order_key(largest(f), uint32_t(base)) >= bound)
+#pragma unroll
+        for (int k = 0; k < N; ++k) take(f[k], base + k, base);
+    }
+  }
+  __syncthreads();
+  const int n = nfound;
+  if (n <= kFound) {
+    by_rank(found, n, a.top, put);
+    for (int k = n + tid; k < a.top; k += NT) put(k, 0);
+    return;
+  }
+  // More elements reach the bound than are kept, as when a thread's elements are all
+  // among the largest: one pass over the segment for each alternative.
+  Key last = ~Key(0);
+  for (int k = 0; k < a.top; ++k) {
+    Key best = 0;
+    auto look = [&](int64_t e) {
+      const float x = T::widen(row.x[e]);
+      const Key key = order_key(x, uint32_t(e));
+      if (x > -kInf && key < last && key > best) best = key;
+    };
+    if (seg == 0 && tid < row.head) look(tid);
+    for (int64_t e = row.head + begin * N + tid; e < row.head + end * N; e += NT) look(e);
+    if (seg == segs - 1 && tid < row.tail) look(a.vocab - row.tail + tid);
+#pragma unroll
+    for (int j = 32; j >= 1; j >>= 1) best = max_key(best, __shfl_xor(best, j, 64));
+    __syncthreads();
+    if (lane == 0) picked[wave] = best;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) best = max_key(best, picked[w]);
+    if (tid == 0) put(k, best);
+    last = best ? best : 1;   // after the last one nothing is below
+  }
+}
+
+// The segments of a row: sums in the order of the segments, alternatives of all of them
+// ranked against each other.
 template <class T>
-__global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(LogprobGradArgs a) {
-  const int64_t t = blockIdx.x, V = a.vocab;
-  const typename T::raw* x = static_cast<const typename T::raw*>(a.logits) + t * a.ld;
-  typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
-  const float lse = a.lse[t];
-  const int64_t tok = a.tokens ? a.tokens[t] : -1;
-  const float g = a.g && tok >= 0 ? a.g[t] : 0.f;
-  const bool outside = a.g && tok >= V;
-  const float h = a.h ? a.h[t] : 0.f, H = a.h ? a.entropy[t] : 0.f;
-  const bool empty = lse == -kInf;
-  for (int64_t v = int64_t(blockIdx.y) * kThreads + threadIdx.x; v < V;
-       v += int64_t(gridDim.y) * kThreads) {
-    const float xv = T::widen(x[v]);
-    const float lp = xv - lse;
-    const float p = expf(lp);
+__global__ void __launch_bounds__(256) logprobs_join_kernel(LogprobArgs a, int segs,
+                                                            const Partial* __restrict__ partial,
+                                                            const Key* __restrict__ seg_top) {
+  __shared__ Key keys[kMaxSegs * kMaxTop];
+  __shared__ int n;
+  const int64_t t = blockIdx.x;
+  const Partial* part = partial + t * segs;
+  float m = part[0].m;
+  for (int s = 1; s < segs; ++s) m = fmaxf(m, part[s].m);
+  double S = 0, E = 0;
+  for (int s = 0; s < segs; ++s) {
+    const float d = fmaxf(part[s].m - m, kFar);
+    const double c = __builtin_amdgcn_exp2f(d * kLog2E);
+    S += c * part[s].S;
+    E += c * (part[s].E + double(d) * part[s].S);
+  }
+  double log_s = S == 0.0 ? -double(kInf) : log(S);
+  if (threadIdx.x == 0) {
+    write_sums<T>(a, t, m, S, E, log_s);
+    n = 0;
+  }
+  if (a.top == 0) return;
+  __syncthreads();
+  // no segment's last alternative is beaten by fewer than `top`
+  const Key* in = seg_top + t * segs * a.top;
+  Key bound = 1;
+  for (int s = 0; s < segs; ++s) bound = max_key(bound, in[s * a.top + a.top - 1]);
+  for (int k = int(threadIdx.x); k < segs * a.top; k += 256)
+    if (in[k] >= bound) keys[atomicAdd(&n, 1)] = in[k];
+  __syncthreads();
+  const int count = S > 0.0 ? n : 0;
+  by_rank(keys, count, a.top, [&](int rank, Key key) { write_alternative(a, t, rank, key, m, log_s); });
+  for (int k = count + int(threadIdx.x); k < a.top; k += 256) write_alternative(a, t, k, 0, m, log_s);
+}
+
+// ---------------------------------------------------------------- gradient
+
+constexpr int kGradThreads = 256;
+
+struct GradRow {
+  float lse, g, h, H;
+  int64_t tok;
+  bool empty, outside;
+  __device__ GradRow(const LogprobGradArgs& a, int64_t t) {
+    lse = a.lse[t];
+    tok = a.tokens ? a.tokens[t] : -1;
+    g = a.g && tok >= 0 ? a.g[t] : 0.f;
+    outside = a.g && tok >= a.vocab;
+    h = a.h ? a.h[t] : 0.f;
+    H = a.h ? a.entropy[t] : 0.f;
+    empty = lse == -kInf;
+  }
+  __device__ __forceinline__ float at(float x, int64_t v) const {
+    const float lp = x - lse;
+    const float p = __builtin_amdgcn_exp2f(lp * kLog2E);
     float d = v == tok ? g : 0.f;
     if (p != 0.f) d -= p * fmaf(h, lp + H, g);   // a NaN counts as different from 0
-    out[v] = T::narrow(outside ? __builtin_nanf("") : empty ? 0.f : d);
+    return outside ? __builtin_nanf("") : empty ? 0.f : d;
   }
+};
+
+// A workgroup takes kUnroll vectors a thread of one row. Logits and gradient may lie
+// differently against 16 bytes: then both go element by element.
+template <class T, bool VECTORS>
+__global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(LogprobGradArgs a) {
+  constexpr int N = Row<T>::N;
+  const int64_t t = blockIdx.x;
+  const typename T::raw* x = static_cast<const typename T::raw*>(a.logits) + t * a.ld;
+  typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
+  const GradRow r(a, t);
+  const int tid = int(threadIdx.x);
+  if constexpr (!VECTORS) {
+    for (int64_t v = int64_t(blockIdx.y) * kGradThreads + tid; v < a.vocab;
+         v += int64_t(gridDim.y) * kGradThreads)
+      out[v] = T::narrow(r.at(T::widen(x[v]), v));
+    return;
+  }
+  const Row<T> row(x, a.vocab);
+  if (blockIdx.y == 0) {
+    if (tid < row.head) out[tid] = T::narrow(r.at(T::widen(x[tid]), tid));
+    const int64_t last = a.vocab - row.tail + tid;
+    if (tid < row.tail) out[last] = T::narrow(r.at(T::widen(x[last]), last));
+  }
+  auto whole = [&](int64_t i, uint4 v) __attribute__((always_inline)) {
+    float f[N];
+    Row<T>::widen(v, f);
+    const int64_t base = row.head + i * N;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = r.at(f[k], base + k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (N == 4) w[k] = __builtin_bit_cast(uint32_t, f[k]);
+      else w[k] = uint32_t(T::narrow(f[2 * k])) | uint32_t(T::narrow(f[2 * k + 1])) << 16;
+    }
+    *reinterpret_cast<uint4*>(out + base) = make_uint4(w[0], w[1], w[2], w[3]);
+  };
+  constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;
+  for (int64_t b = int64_t(blockIdx.y) * kStep; b < row.vectors; b += int64_t(gridDim.y) * kStep) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t i = b + u * kGradThreads + tid;
+      if (i < row.vectors) v[u] = row.load(i);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t i = b + u * kGradThreads + tid;
+      if (i < row.vectors) whole(i, v[u]);
+    }
+  }
+}
+
+size_t partial_bytes(int64_t nrows, int segs) {
+  return align256(size_t(nrows) * segs * sizeof(Partial));
+}
+
+// Segments of a row.
+int segments(int64_t nrows, int64_t vocab) {
+  if (nrows >= 256) return 1;
+  const int64_t want = std::min<int64_t>(512 / nrows, vocab / 32768);
+  return int(std::max<int64_t>(1, std::min<int64_t>(want, kMaxSegs)));
 }
 
 }  // namespace
 
-size_t token_logprobs_workspace_bytes(int64_t, int64_t, int) { return 0; }
+size_t token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int top) {
+  const int segs = segments(nrows, vocab);
+  if (segs == 1) return 0;
+  return partial_bytes(nrows, segs) + align256(size_t(nrows) * segs * top * sizeof(Key));
+}
 
-hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void*, hipStream_t stream) {
+hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void* d_ws, hipStream_t stream) {
+  const int segs = segments(a.nrows, a.vocab);
+  const dim3 grid(unsigned(a.nrows), unsigned(segs));
+  Partial* part = static_cast<Partial*>(d_ws);
+  Key* keys = reinterpret_cast<Key*>(static_cast<char*>(d_ws) + partial_bytes(a.nrows, segs));
   return with_type(type, [&](auto t) {
-    hipLaunchKernelGGL(logprobs_kernel<decltype(t)>, dim3(unsigned(a.nrows)), dim3(kThreads), 0,
-                       stream, a);
+    using T = decltype(t);
+    const int64_t per = a.vocab / segs;
+    if (per <= 2048)
+      hipLaunchKernelGGL((logprobs_kernel<T, 64>), grid, dim3(64), 0, stream, a, segs, part, keys);
+    else if (per <= 8192 || a.nrows * segs >= 512)
+      hipLaunchKernelGGL((logprobs_kernel<T, 256>), grid, dim3(256), 0, stream, a, segs, part, keys);
+    else
+      hipLaunchKernelGGL((logprobs_kernel<T, 1024>), grid, dim3(1024), 0, stream, a, segs, part, keys);
+    if (segs > 1)
+      hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(unsigned(a.nrows)), dim3(256), 0, stream, a,
+                         segs, part, keys);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_token_logprobs_backward(const LogprobGradArgs& a, int type, hipStream_t stream) {
-  const int64_t parts = std::min<int64_t>((a.vocab + 8 * kThreads - 1) / (8 * kThreads), 65535);
   return with_type(type, [&](auto t) {
-    hipLaunchKernelGGL(logprobs_backward_kernel<decltype(t)>,
-                       dim3(unsigned(a.nrows), unsigned(parts)), dim3(kThreads), 0, stream, a);
+    using T = decltype(t);
+    using raw = typename T::raw;
+    const int64_t step = int64_t(kUnroll) * kGradThreads * Row<T>::N;
+    const dim3 grid(unsigned(a.nrows),
+                    unsigned(std::min<int64_t>((a.vocab + step - 1) / step, 65535)));
+    const auto off = [](const void* p) { return reinterpret_cast<uintptr_t>(p) & 15u; };
+    const bool vectors = off(a.logits) == off(a.grad) &&
+                         (a.nrows == 1 || uint64_t(a.ld - a.ldg) * sizeof(raw) % 16 == 0);
+    if (vectors)
+      hipLaunchKernelGGL((logprobs_backward_kernel<T, true>), grid, dim3(kGradThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((logprobs_backward_kernel<T, false>), grid, dim3(kGradThreads), 0, stream, a);
     return hipGetLastError();
   });
 }
