@@ -38,35 +38,15 @@ __device__ __forceinline__ float key_value(Key key) {
 __device__ __forceinline__ uint32_t key_index(Key key) { return 0xFFFFFFFFu - uint32_t(key); }
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 
-// A row in 16-byte vectors: `head` elements before the first boundary, then vectors,
-// then the rest.
+// A row in 16-byte vectors and the elements after the last.
 template <class T>
 struct Row {
-  static constexpr int N = 16 / sizeof(typename T::raw);
+  static constexpr int N = kPerVector<T>;
   const typename T::raw* x;
   int64_t vectors;
-  int head, tail;
-  __device__ Row(const typename T::raw* p, int64_t n) : x(p) {
-    const int64_t h = int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(*p);
-    head = int(std::min<int64_t>(h, n));
-    vectors = (n - head) / N;
-    tail = int(n - head - vectors * N);
-  }
-  __device__ __forceinline__ uint4 load(int64_t i) const {
-    return *reinterpret_cast<const uint4*>(x + head + i * N);
-  }
-  __device__ static __forceinline__ void widen(uint4 v, float (&f)[N]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (N == 4) {
-        f[i] = __builtin_bit_cast(float, w[i]);
-      } else {
-        f[2 * i] = T::widen(uint16_t(w[i] & 0xFFFFu));
-        f[2 * i + 1] = T::widen(uint16_t(w[i] >> 16));
-      }
-    }
-  }
+  int tail;
+  __device__ Row(const typename T::raw* p, int64_t n) : x(p), vectors(n / N), tail(int(n % N)) {}
+  __device__ __forceinline__ uint32x4 load(int64_t i) const { return load16(x + i * N); }
 };
 
 struct Sums {
@@ -159,7 +139,7 @@ __device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
 // it. The top-th largest of these over the threads (found in two steps, over 64 groups of
 // threads and over the threads of the groups that reach it) bounds the top-th largest
 // element from below, so only vectors of the at most kMaxTop threads that reach the
-// bound are read again, each thread's by its whole wave, and the elements that reach it
+// bound are read again, by all threads together, and the elements that reach it
 // are ranked against each other. Vectors are intervals of the row, so the order of
 // (value, first vector) is that of (value, index), and ties are cut the same way.
 template <class T, int NT>
@@ -169,7 +149,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
   constexpr int N = Row<T>::N, kWaves = NT / 64, kGroup = NT / 64;
   __shared__ double sd[2][kWaves];
   __shared__ float sf[kWaves];
-  __shared__ Key group_key[64], picked[kPicked], found[kFound], cut;
+  __shared__ Key group_key[64], picked[kPicked], chosen[kMaxTop], found[kFound];
   __shared__ int npicked, nfound;
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
@@ -183,18 +163,17 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
     s.add(x);
     s.note(x, uint32_t(i));
   };
-  if (seg == 0 && tid < row.head) one(tid);
   int64_t i = begin + tid;
   for (; i + (kUnroll - 1) * NT < end; i += kUnroll * NT) {
-    uint4 v[kUnroll];
+    uint32x4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) v[u] = row.load(i + u * NT);
     float f[kUnroll][N], top = -kInf;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      Row<T>::widen(v[u], f[u]);
+      widen<T>(v[u], f[u]);
       const float l = largest(f[u]);
-      s.note(l, uint32_t(row.head + (i + u * NT) * N));
+      s.note(l, uint32_t((i + u * NT) * N));
       top = fmaxf(top, l);
     }
     s.raise(top);
@@ -205,9 +184,9 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
   }
   for (; i < end; i += NT) {
     float f[N];
-    Row<T>::widen(row.load(i), f);
+    widen<T>(row.load(i), f);
     const float l = largest(f);
-    s.note(l, uint32_t(row.head + i * N));
+    s.note(l, uint32_t(i * N));
     s.raise(l);
 #pragma unroll
     for (int k = 0; k < N; ++k) s.add(f[k]);
@@ -215,34 +194,23 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
   if (seg == segs - 1 && tid < row.tail) one(a.vocab - row.tail + tid);
 
   // the sums of the threads
-  float m = s.m;
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  float m = lanes_reduce(s.m, [](float p, float q) { return fmaxf(p, q); });
   if (lane == 0) sf[wave] = m;
-  if (tid == 0) {
-    npicked = nfound = 0;
-    cut = 1;
-  }
+  if (tid == 0) npicked = nfound = 0;
   __syncthreads();
   m = sf[0];
   for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sf[w]);
   const float d = fmaxf(s.m - m, kFar);
   const double c = __builtin_amdgcn_exp2f(d * kLog2E);
-  double S = c * s.S, E = c * (s.E + double(d) * s.S);
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) {
-    S += __shfl_xor(S, k, 64);
-    E += __shfl_xor(E, k, 64);
-  }
+  const auto add = [](double p, double q) { return p + q; };
+  double S = lanes_reduce(c * s.S, add), E = lanes_reduce(c * (s.E + double(d) * s.S), add);
   if (lane == 0) {
     sd[0][wave] = S;
     sd[1][wave] = E;
   }
   // the largest element of each of 64 groups of threads
   const Key mine = s.best > -kInf ? order_key(s.best, s.base) : 0;
-  Key g = mine;
-#pragma unroll
-  for (int k = 1; k < kGroup; k <<= 1) g = max_key(g, __shfl_xor(g, k, 64));
+  const Key g = lanes_reduce<kGroup>(mine, max_key);
   if (tid % kGroup == 0) group_key[tid / kGroup] = g;
   __syncthreads();
   S = sd[0][0], E = sd[1][0];
@@ -276,32 +244,34 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
     if (mine && mine >= bound) picked[atomicAdd(&npicked, 1)] = mine;
   }
   __syncthreads();
-  by_rank(picked, npicked, a.top, [&](int rank, Key key) {
-    if (rank == a.top - 1) cut = key;
-  });
+  const int nchosen = std::min(npicked, a.top);
+  by_rank(picked, npicked, a.top, [&](int rank, Key key) { chosen[rank] = key; });
   __syncthreads();
-  const Key bound = cut;
+  const Key bound = npicked < a.top ? 1 : chosen[a.top - 1];
   auto take = [&](float x, int64_t index, int64_t base) {
     if (x > -kInf && order_key(x, uint32_t(base)) >= bound) {
       const int k = atomicAdd(&nfound, 1);
       if (k < kFound) found[k] = order_key(x, uint32_t(index));
     }
   };
-  if (mine >= bound) {   // its single elements
-    if (seg == 0 && tid < row.head) take(T::widen(row.x[tid]), tid, tid);
-    const int64_t last = a.vocab - row.tail + tid;
-    if (seg == segs - 1 && tid < row.tail) take(T::widen(row.x[last]), last, last);
-  }
-  for (unsigned long long todo = __ballot(mine >= bound); todo; todo &= todo - 1) {
-    const int64_t first = begin + wave * 64 + __builtin_ctzll(todo);
-    for (int64_t v = first + int64_t(lane) * NT; v < end; v += int64_t(64) * NT) {
-      float f[N];
-      Row<T>::widen(row.load(v), f);
-      const int64_t base = row.head + v * N;
-      if (order_key(largest(f), uint32_t(base)) >= bound)
-#pragma unroll
-        for (int k = 0; k < N; ++k) take(f[k], base + k, base);
+  // all threads over (chosen thread, its vectors and its element after the last)
+  const uint32_t each = uint32_t((end - begin + NT - 1) / NT) + 1;
+  for (uint32_t p = uint32_t(tid); p < uint32_t(nchosen) * each; p += NT) {
+    const uint32_t step = p % each;
+    const int64_t first = key_index(chosen[p / each]), after = row.vectors * N;
+    const int64_t owner = first < after ? (first / N - begin) % NT : first - after;
+    if (step == each - 1) {
+      const int64_t e = after + owner;
+      if (seg == segs - 1 && owner < row.tail) take(T::widen(row.x[e]), e, e);
+      continue;
     }
+    const int64_t v = begin + owner + int64_t(step) * NT;
+    if (v >= end) continue;
+    float f[N];
+    widen<T>(row.load(v), f);
+    if (order_key(largest(f), uint32_t(v * N)) >= bound)
+#pragma unroll
+      for (int k = 0; k < N; ++k) take(f[k], v * N + k, v * N);
   }
   __syncthreads();
   const int n = nfound;
@@ -320,11 +290,9 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
       const Key key = order_key(x, uint32_t(e));
       if (x > -kInf && key < last && key > best) best = key;
     };
-    if (seg == 0 && tid < row.head) look(tid);
-    for (int64_t e = row.head + begin * N + tid; e < row.head + end * N; e += NT) look(e);
+    for (int64_t e = begin * N + tid; e < end * N; e += NT) look(e);
     if (seg == segs - 1 && tid < row.tail) look(a.vocab - row.tail + tid);
-#pragma unroll
-    for (int j = 32; j >= 1; j >>= 1) best = max_key(best, __shfl_xor(best, j, 64));
+    best = lanes_reduce(best, max_key);
     __syncthreads();
     if (lane == 0) picked[wave] = best;
     __syncthreads();
@@ -398,45 +366,22 @@ struct GradRow {
   }
 };
 
-// A workgroup takes kUnroll vectors a thread of one row. Logits and gradient may lie
-// differently against 16 bytes: then both go element by element.
-template <class T, bool VECTORS>
+// A workgroup takes kUnroll vectors a thread of one row at a time.
+template <class T>
 __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(LogprobGradArgs a) {
-  constexpr int N = Row<T>::N;
+  constexpr int N = kPerVector<T>;
   const int64_t t = blockIdx.x;
-  const typename T::raw* x = static_cast<const typename T::raw*>(a.logits) + t * a.ld;
+  const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
   typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
   const GradRow r(a, t);
   const int tid = int(threadIdx.x);
-  if constexpr (!VECTORS) {
-    for (int64_t v = int64_t(blockIdx.y) * kGradThreads + tid; v < a.vocab;
-         v += int64_t(gridDim.y) * kGradThreads)
-      out[v] = T::narrow(r.at(T::widen(x[v]), v));
-    return;
+  if (blockIdx.y == 0 && tid < row.tail) {
+    const int64_t e = row.vectors * N + tid;
+    out[e] = T::narrow(r.at(T::widen(row.x[e]), e));
   }
-  const Row<T> row(x, a.vocab);
-  if (blockIdx.y == 0) {
-    if (tid < row.head) out[tid] = T::narrow(r.at(T::widen(x[tid]), tid));
-    const int64_t last = a.vocab - row.tail + tid;
-    if (tid < row.tail) out[last] = T::narrow(r.at(T::widen(x[last]), last));
-  }
-  auto whole = [&](int64_t i, uint4 v) __attribute__((always_inline)) {
-    float f[N];
-    Row<T>::widen(v, f);
-    const int64_t base = row.head + i * N;
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < N; ++k) f[k] = r.at(f[k], base + k);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (N == 4) w[k] = __builtin_bit_cast(uint32_t, f[k]);
-      else w[k] = uint32_t(T::narrow(f[2 * k])) | uint32_t(T::narrow(f[2 * k + 1])) << 16;
-    }
-    *reinterpret_cast<uint4*>(out + base) = make_uint4(w[0], w[1], w[2], w[3]);
-  };
   constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;
   for (int64_t b = int64_t(blockIdx.y) * kStep; b < row.vectors; b += int64_t(gridDim.y) * kStep) {
-    uint4 v[kUnroll];
+    uint32x4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t i = b + u * kGradThreads + tid;
@@ -445,7 +390,12 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(Logprob
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t i = b + u * kGradThreads + tid;
-      if (i < row.vectors) whole(i, v[u]);
+      if (i >= row.vectors) break;
+      float f[N];
+      widen<T>(v[u], f);
+#pragma unroll
+      for (int k = 0; k < N; ++k) f[k] = r.at(f[k], i * N + k);
+      store16(out + i * N, narrow<T>(f));
     }
   }
 }
@@ -493,17 +443,10 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void* d_ws, hip
 hipError_t launch_token_logprobs_backward(const LogprobGradArgs& a, int type, hipStream_t stream) {
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    using raw = typename T::raw;
-    const int64_t step = int64_t(kUnroll) * kGradThreads * Row<T>::N;
+    const int64_t step = int64_t(kUnroll) * kGradThreads * kPerVector<T>;
     const dim3 grid(unsigned(a.nrows),
                     unsigned(std::min<int64_t>((a.vocab + step - 1) / step, 65535)));
-    const auto off = [](const void* p) { return reinterpret_cast<uintptr_t>(p) & 15u; };
-    const bool vectors = off(a.logits) == off(a.grad) &&
-                         (a.nrows == 1 || uint64_t(a.ld - a.ldg) * sizeof(raw) % 16 == 0);
-    if (vectors)
-      hipLaunchKernelGGL((logprobs_backward_kernel<T, true>), grid, dim3(kGradThreads), 0, stream, a);
-    else
-      hipLaunchKernelGGL((logprobs_backward_kernel<T, false>), grid, dim3(kGradThreads), 0, stream, a);
+    hipLaunchKernelGGL(logprobs_backward_kernel<T>, grid, dim3(kGradThreads), 0, stream, a);
     return hipGetLastError();
   });
 }

@@ -29,43 +29,89 @@ struct BF16 {
   }
 };
 
-// Eight consecutive elements widened to fp32: one or two 16-byte loads where the
-// caller knows the address to be 16-byte aligned, else eight loads.
-template <class T, bool ALIGNED>
-__device__ __forceinline__ void load8(const typename T::raw* p, float (&f)[8]) {
-  if constexpr (!ALIGNED) {
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
+// 16 bytes at any element: global loads and stores of vectors need no alignment here.
+typedef uint32x4 uint32x4_any __attribute__((aligned(2)));
+
+__device__ __forceinline__ uint32x4 load16(const void* p) {
+  return *static_cast<const uint32x4_any*>(p);
+}
+__device__ __forceinline__ void store16(void* p, uint32x4 v) { *static_cast<uint32x4_any*>(p) = v; }
+
+// The elements of a vector in fp32, and back.
+template <class T>
+constexpr int kPerVector = 16 / sizeof(typename T::raw);
+
+template <class T>
+__device__ __forceinline__ void widen(uint32x4 v, float* f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = T::widen(p[i]);
-  } else if constexpr (sizeof(typename T::raw) == 4) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
-    f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-  } else {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = T::widen(uint16_t(w[i] & 0xFFFFu));
-      f[2 * i + 1] = T::widen(uint16_t(w[i] >> 16));
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = v[i];
+    if constexpr (kPerVector<T> == 4) {
+      f[i] = __builtin_bit_cast(float, w);
+    } else {
+      f[2 * i] = T::widen(uint16_t(w & 0xFFFFu));
+      f[2 * i + 1] = T::widen(uint16_t(w >> 16));
     }
   }
 }
-
-template <class T, bool ALIGNED>
-__device__ __forceinline__ void store8(typename T::raw* p, const float (&f)[8]) {
-  if constexpr (!ALIGNED) {
+template <class T>
+__device__ __forceinline__ uint32x4 narrow(const float* f) {
+  uint32x4 v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = T::narrow(f[i]);
-  } else if constexpr (sizeof(typename T::raw) == 4) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = uint32_t(T::narrow(f[2 * i])) | uint32_t(T::narrow(f[2 * i + 1])) << 16;
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kPerVector<T> == 4) v[i] = __builtin_bit_cast(uint32_t, f[i]);
+    else v[i] = uint32_t(T::narrow(f[2 * i])) | uint32_t(T::narrow(f[2 * i + 1])) << 16;
   }
+  return v;
+}
+
+// Eight consecutive elements.
+template <class T>
+__device__ __forceinline__ void load8(const typename T::raw* p, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += kPerVector<T>) widen<T>(load16(p + i), f + i);
+}
+template <class T>
+__device__ __forceinline__ void store8(typename T::raw* p, const float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += kPerVector<T>) store16(p + i, narrow<T>(f + i));
+}
+
+// f over `LANES` neighbouring lanes (a power of two), the result in all of them; f
+// commutes, so it is the same in all. Steps within 16 lanes are data-parallel moves (the
+// mirrored ones meet a half whose lanes all hold the same), those across exchange rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, true));
+}
+template <class V, class F>
+__device__ __forceinline__ V apart(V v, F f) {   // f on the 32-bit words of v
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two words");
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, f(__builtin_bit_cast(uint32_t, v)));
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(V, uint64_t(f(uint32_t(u))) | uint64_t(f(uint32_t(u >> 32))) << 32);
+  }
+}
+template <int LANES = 64, class V, class F>
+__device__ __forceinline__ V lanes_reduce(V v, F f) {
+  if constexpr (LANES >= 2) v = f(v, apart(v, [](uint32_t w) { return moved<0xB1>(w); }));
+  if constexpr (LANES >= 4) v = f(v, apart(v, [](uint32_t w) { return moved<0x4E>(w); }));
+  if constexpr (LANES >= 8) v = f(v, apart(v, [](uint32_t w) { return moved<0x141>(w); }));
+  if constexpr (LANES >= 16) v = f(v, apart(v, [](uint32_t w) { return moved<0x140>(w); }));
+  if constexpr (LANES >= 32) {
+    const V a = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[0]; });
+    const V b = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[1]; });
+    v = f(a, b);
+  }
+  if constexpr (LANES >= 64) {
+    const V a = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[0]; });
+    const V b = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[1]; });
+    v = f(a, b);
+  }
+  return v;
 }
 
 // Calls f with the element type of a SEEDQ_* type code (checked by the caller).
@@ -77,11 +123,6 @@ inline hipError_t with_type(int type, F f) {
     case SEEDQ_BF16: return f(BF16{});
     default: return hipErrorInvalidValue;
   }
-}
-
-// 16-byte aligned rows of elements of `size` bytes.
-inline bool rows_aligned(const void* p, int64_t ld, size_t size) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (uint64_t(ld) * size) % 16 == 0;
 }
 
 }  // namespace seedq

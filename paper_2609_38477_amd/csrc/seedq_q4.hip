@@ -22,7 +22,7 @@ __device__ __forceinline__ float rounded_quotient(float w, float s, float inv) {
   return q;
 }
 
-template <class T, bool ALIGNED, bool ZEROS>
+template <class T, bool ZEROS>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, int64_t nrows, int64_t ncols,
                 int64_t row_words, int64_t ngroups, int gshift, uint32_t tiles, int64_t total,
@@ -34,7 +34,7 @@ quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, int64_t nrow
   const int64_t r = int64_t(uint32_t(job) / tiles);
   const int64_t word = int64_t(uint32_t(job) % tiles) * 64 + lane, c = word * 8;
   float w[8] = {};
-  if (c < ncols) load8<T, ALIGNED>(W + r * ldw + c, w);
+  if (c < ncols) load8<T>(W + r * ldw + c, w);
   float lo = 0.f, hi = 0.f;
   uint32_t big = 0;   // the largest pattern without sign: above 0x7F7FFFFF it is not finite
 #pragma unroll
@@ -76,7 +76,7 @@ quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, int64_t nrow
   }
 }
 
-template <class T, bool ALIGNED>
+template <class T>
 __global__ void __launch_bounds__(kThreads)
 dequantize_kernel(Q4 q, uint32_t tiles, int64_t total, typename T::raw* __restrict__ W,
                   int64_t ldw) {
@@ -93,7 +93,7 @@ dequantize_kernel(Q4 q, uint32_t tiles, int64_t total, typename T::raw* __restri
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (float((code >> (4 * i)) & 15u) - z) * s;
-  store8<T, ALIGNED>(W + r * ldw + c, f);
+  store8<T>(W + r * ldw + c, f);
 }
 
 // Jobs of one wave: 64 words of one row.
@@ -125,9 +125,7 @@ hipError_t launch_q4_quantize(const void* d_W, int type, int64_t ldw, int64_t nr
                          ldw, nrows, ncols, row_words, ngroups, gshift, j.tiles, j.total, d_codes,
                          d_scale, d_zero);
     };
-    const bool al = rows_aligned(d_W, ldw, sizeof(raw));
-    if (d_zero) al ? launch(quantize_kernel<T, true, true>) : launch(quantize_kernel<T, false, true>);
-    else al ? launch(quantize_kernel<T, true, false>) : launch(quantize_kernel<T, false, false>);
+    d_zero ? launch(quantize_kernel<T, true>) : launch(quantize_kernel<T, false>);
     return hipGetLastError();
   });
 }
@@ -138,12 +136,8 @@ hipError_t launch_q4_dequantize(const Q4& q, void* d_W_hat, int type, int64_t ld
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     using raw = typename T::raw;
-    auto launch = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3(j.grid), dim3(kThreads), 0, stream, q, j.tiles, j.total,
-                         static_cast<raw*>(d_W_hat), ldw);
-    };
-    rows_aligned(d_W_hat, ldw, sizeof(raw)) ? launch(dequantize_kernel<T, true>)
-                                            : launch(dequantize_kernel<T, false>);
+    hipLaunchKernelGGL(dequantize_kernel<T>, dim3(j.grid), dim3(kThreads), 0, stream, q, j.tiles,
+                       j.total, static_cast<raw*>(d_W_hat), ldw);
     return hipGetLastError();
   });
 }

@@ -22,7 +22,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kCodeScale = 512.f;   // 2^9
 
@@ -82,15 +81,6 @@ __device__ __forceinline__ uint32x4 to_code_order(uint32x4 d) {
                   __builtin_amdgcn_perm(d[3], d[2], 0x07060302u)};
 }
 
-// Eight 16-bit elements as they lie; `aligned` to 16 bytes is the same for all lanes.
-__device__ __forceinline__ uint32x4 load8_raw(const uint16_t* p, bool aligned) {
-  if (aligned) return *reinterpret_cast<const uint32x4*>(p);
-  uint32x4 d;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) d[i] = uint32_t(p[2 * i]) | uint32_t(p[2 * i + 1]) << 16;
-  return d;
-}
-
 // Eight fp32 values as three bf16 pieces in code order.
 __device__ __forceinline__ void split8(const float (&f)[8], uint32x4 (&piece)[3]) {
   uint32_t h[3][8];
@@ -128,7 +118,7 @@ constexpr int kMaxWaves = 16;
 
 template <class X, int NV, int WORDS>
 __global__ void __launch_bounds__(64 * kMaxWaves)
-gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, bool aligned, int slabs,
+gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int slabs,
                 void* __restrict__ y, int ytype, int64_t ldy) {
   __shared__ float part[kMaxWaves][NV][kRows];
   const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), waves = int(blockDim.x >> 6);
@@ -165,7 +155,7 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, bool a
         const typename X::raw* xv = x + v * ldx + c;
 #pragma unroll
         for (int i = 0; i < 8; ++i) xf[v][w][i] = 0.f;
-        if (c < q.ncols) aligned ? load8<X, true>(xv, xf[v][w]) : load8<X, false>(xv, xf[v][w]);
+        if (c < q.ncols) load8<X>(xv, xf[v][w]);
       }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
@@ -221,16 +211,13 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, bool a
 // x in fp32 as three bf16 rows a vector (row 3 v + p), in code order, zeros from ncols
 // to the padded end of the codes' rows.
 __global__ void __launch_bounds__(256)
-split_kernel(const float* __restrict__ x, int64_t ldx, bool aligned, int64_t ncols, int64_t row_words,
+split_kernel(const float* __restrict__ x, int64_t ldx, int64_t ncols, int64_t row_words,
              uint16_t* __restrict__ out) {
   const int64_t v = blockIdx.y;
   const int64_t w = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (w >= row_words) return;
   float f[8] = {};
-  if (w * kC < ncols) {
-    const float* p = x + v * ldx + w * kC;
-    aligned ? load8<F32, true>(p, f) : load8<F32, false>(p, f);
-  }
+  if (w * kC < ncols) load8<F32>(x + v * ldx + w * kC, f);
   uint32x4 piece[3];
   split8(f, piece);
 #pragma unroll
@@ -255,7 +242,7 @@ struct Chunk {
 
 template <class M, int P, int NG, int RT, int MT>
 __global__ void __launch_bounds__(64 * kMaxWaves / (MT == 4 ? 2 : 1))
-gemv_batch_kernel(Q4 q, int64_t nvec, const uint16_t* __restrict__ x, int64_t ldx, bool aligned,
+gemv_batch_kernel(Q4 q, int64_t nvec, const uint16_t* __restrict__ x, int64_t ldx,
                   void* __restrict__ y, int ytype, int64_t ldy) {
   constexpr int kVec = 16 * MT / P;   // vectors of a workgroup
   extern __shared__ float part[];
@@ -297,7 +284,7 @@ gemv_batch_kernel(Q4 q, int64_t nvec, const uint16_t* __restrict__ x, int64_t ld
       for (int t = 0; t < 4; ++t) {
         const int64_t k = ch * 128 + (NG == 1 ? kg * 32 + t * 8 : t * 32 + kg * 8);
         c.x[m][t] = uint32x4{0u, 0u, 0u, 0u};
-        if (k < xcols) c.x[m][t] = load8_raw(xrow[m] + k, aligned);
+        if (k < xcols) c.x[m][t] = load16(xrow[m] + k);
       }
   };
   floatx4 sum[RT][MT] = {};
@@ -381,14 +368,13 @@ hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, v
                       int64_t ldy, hipStream_t stream) {
   using raw = typename X::raw;
   const int64_t words = (q.ncols + kC - 1) / kC;
-  const bool al = rows_aligned(d_x, ldx, sizeof(raw));
   const unsigned grid = unsigned((q.nrows + kRows - 1) / kRows);
   const int per = words > 128 ? 4 : words > 64 ? 2 : 1;
   const int slabs = int((words + 64 * per - 1) / (64 * per));
   const int waves = std::min(slabs, kMaxWaves);
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), 0, stream, q, static_cast<const raw*>(d_x),
-                       ldx, al, slabs, d_y, ytype, ldy);
+                       ldx, slabs, d_y, ytype, ldy);
     return hipGetLastError();
   };
   auto words_of = [&](auto nv) {
@@ -402,7 +388,7 @@ hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, v
 }
 
 template <class M, int P>
-hipError_t launch_batch(const Q4& q, int64_t nvec, const uint16_t* x, int64_t ldx, bool aligned,
+hipError_t launch_batch(const Q4& q, int64_t nvec, const uint16_t* x, int64_t ldx,
                         void* d_y, int ytype, int64_t ldy, hipStream_t stream) {
   const int64_t rows = nvec * P, chunks = (q.ncols + 127) / 128;
   auto go = [&](auto ng, auto rt, auto mt) {
@@ -413,7 +399,7 @@ hipError_t launch_batch(const Q4& q, int64_t nvec, const uint16_t* x, int64_t ld
       const int64_t n = std::min<int64_t>(65535 * kVec, nvec - v);
       const dim3 grid(unsigned((q.nrows + 16 * RT - 1) / (16 * RT)), unsigned((n + kVec - 1) / kVec));
       hipLaunchKernelGGL((gemv_batch_kernel<M, P, NG, RT, MT>), grid, dim3(64 * waves),
-                         size_t(waves) * RT * MT * 1024, stream, q, n, x + v * P * ldx, ldx, aligned,
+                         size_t(waves) * RT * MT * 1024, stream, q, n, x + v * P * ldx, ldx,
                          static_cast<char*>(d_y) + v * ldy * (ytype == SEEDQ_F32 ? 4 : 2), ytype, ldy);
     }
     return hipGetLastError();
@@ -447,19 +433,17 @@ hipError_t launch_q4_gemv(const Q4& q, int64_t nvec, const void* d_x, int xtype,
     });
   if (xtype == SEEDQ_F32) {
     uint16_t* pieces = static_cast<uint16_t*>(d_ws);
-    const bool al = rows_aligned(d_x, ldx, 4);
     for (int64_t v = 0; v < nvec; v += 65535) {   // the grid's second dimension has 16 bits
       const int64_t n = std::min<int64_t>(65535, nvec - v);
       hipLaunchKernelGGL(split_kernel, dim3(unsigned((q.row_words + 255) / 256), unsigned(n)),
-                         dim3(256), 0, stream, static_cast<const float*>(d_x) + v * ldx, ldx, al,
+                         dim3(256), 0, stream, static_cast<const float*>(d_x) + v * ldx, ldx,
                          q.ncols, q.row_words, pieces + v * 3 * q.row_words * kC);
     }
-    return launch_batch<Brain, 3>(q, nvec, pieces, q.row_words * kC, true, d_y, ytype, ldy, stream);
+    return launch_batch<Brain, 3>(q, nvec, pieces, q.row_words * kC, d_y, ytype, ldy, stream);
   }
-  const bool al = rows_aligned(d_x, ldx, 2);
   const uint16_t* x = static_cast<const uint16_t*>(d_x);
-  return xtype == SEEDQ_F16 ? launch_batch<Half, 1>(q, nvec, x, ldx, al, d_y, ytype, ldy, stream)
-                            : launch_batch<Brain, 1>(q, nvec, x, ldx, al, d_y, ytype, ldy, stream);
+  return xtype == SEEDQ_F16 ? launch_batch<Half, 1>(q, nvec, x, ldx, d_y, ytype, ldy, stream)
+                            : launch_batch<Brain, 1>(q, nvec, x, ldx, d_y, ytype, ldy, stream);
 }
 
 }  // namespace seedq
