@@ -20,9 +20,8 @@ constexpr float kLog2E = 1.44269504088896340736f;
 constexpr float kFar = -1e30f;      // stands in for x - m = -inf: its e^ is 0, and so is 0 x kFar
 constexpr int kUnroll = 4;          // vectors in flight a thread
 constexpr int kMaxTop = SEEDQ_MAX_TOP;
-constexpr int kPicked = 512;        // threads that may hold an alternative: kMaxTop groups of 16
-constexpr int kFound = 1024;        // elements collected before the slow selection steps in
-constexpr int kMaxSegs = 32;
+constexpr int kManyPicked = 2 * kMaxTop;
+constexpr int kMaxSegs = 16;
 
 // Order of alternatives in one number: the value's pattern made monotonic (-0 is
 // 0), then the lower index first. 0 stands for none.
@@ -43,11 +42,17 @@ template <class T>
 struct Row {
   static constexpr int N = kPerVector<T>;
   const typename T::raw* x;
-  int64_t vectors;
-  int tail;
-  __device__ Row(const typename T::raw* p, int64_t n) : x(p), vectors(n / N), tail(int(n % N)) {}
-  __device__ __forceinline__ uint32x4 load(int64_t i) const { return load16(x + i * N); }
+  uint32_t vectors, tail;   // a row has fewer than 2^31 elements
+  __device__ Row(const typename T::raw* p, int64_t n)
+      : x(p), vectors(uint32_t(n) / N), tail(uint32_t(n) % N) {}
+  __device__ __forceinline__ uint32x4 load(uint32_t i) const { return load16(x + size_t(i) * N); }
 };
+
+template <class T>
+__device__ __forceinline__ uint32x4 minus_infinity() {
+  const uint32_t w = kPerVector<T> == 4 ? 0xFF800000u : uint32_t(T::narrow(-kInf)) * 0x10001u;
+  return uint32x4{w, w, w, w};
+}
 
 struct Sums {
   float m = -FLT_MAX, S = 0.f, E = 0.f;
@@ -92,23 +97,26 @@ struct Partial {
   float m, unused;
 };
 
-// The outputs of row t but for the alternatives, by one thread.
+// The logit of a row's token. It is asked for before the sums meet, so that it is there
+// when they have.
 template <class T>
-__device__ void write_sums(const LogprobArgs& a, int64_t t, float m, double S, double E, double& log_s) {
-  const double nan = __builtin_nan("");
+__device__ __forceinline__ float token_logit(const LogprobArgs& a, int64_t t, int64_t tok) {
+  const typename T::raw* x = static_cast<const typename T::raw*>(a.logits) + t * a.ld;
+  return T::widen(x[tok >= 0 && tok < a.vocab ? tok : 0]);
+}
+
+// log S; S is 0 in a row without a finite logit and NaN in one without a distribution.
+__device__ __forceinline__ double log_of(double S) { return S == 0.0 ? -double(kInf) : log(S); }
+
+// The outputs of row t but for the alternatives, by one thread.
+__device__ __forceinline__ void write_sums(const LogprobArgs& a, int64_t t, int64_t tok, float x,
+                                           float m, double S, double E, double log_s) {
   const bool empty = S == 0.0;
-  log_s = empty ? -double(kInf) : log(S);   // NaN where S is
   if (a.lse) a.lse[t] = empty ? -kInf : float(double(m) + log_s);
   if (a.entropy) a.entropy[t] = empty ? 0.f : float(log_s - E / S);
   if (a.logprob) {
-    const int64_t tok = a.tokens[t];
-    double lp = 0.0;
-    if (tok >= a.vocab) lp = nan;
-    else if (tok >= 0) {
-      const float x = T::widen(static_cast<const typename T::raw*>(a.logits)[t * a.ld + tok]);
-      lp = empty ? -double(kInf) : (double(x) - m) - log_s;
-    }
-    a.logprob[t] = float(lp);
+    const double lp = empty ? -double(kInf) : (double(x) - m) - log_s;
+    a.logprob[t] = tok < 0 ? 0.f : tok >= a.vocab ? __builtin_nanf("") : float(lp);
   }
 }
 
@@ -127,6 +135,7 @@ __device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
   for (int i = int(threadIdx.x); i < n; i += int(blockDim.x)) {
     const Key mine = list[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
     if (rank < top) f(rank, mine);
   }
@@ -135,64 +144,69 @@ __device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
 // One workgroup of NT threads a row, or a segment of one (blockIdx.y of segs), whose
 // sums and alternatives then go to the join.
 //
-// Alternatives: each thread remembers its largest element and the vector that first had
-// it. The top-th largest of these over the threads (found in two steps, over 64 groups of
-// threads and over the threads of the groups that reach it) bounds the top-th largest
-// element from below, so only vectors of the at most kMaxTop threads that reach the
-// bound are read again, by all threads together, and the elements that reach it
-// are ranked against each other. Vectors are intervals of the row, so the order of
-// (value, first vector) is that of (value, index), and ties are cut the same way.
+// Alternatives: a thread remembers its largest element and the vector that first had it.
+// The top-th largest of the largest keys of 64 groups of threads bounds the top-th
+// largest element from below (where many keys reach it, as among equal logits, the
+// top-th largest key takes its place), so only the vectors of threads whose keys reach
+// the bound are read again, by all threads together, and the elements that reach it are
+// ranked against each other. Vectors are intervals of the row, so the order of (value,
+// first vector) is that of (value, index), and ties are cut the same way. A thread's
+// vectors lie in as many cache lines, which is what the second look costs: 2048 rows of
+// 131072 bf16 logits take 109 us with 5 alternatives, 118 with 20 and 110 with none. For
+// few rows the launch spends its time on the way through the code, so that is kept short:
+// one row of 32000 fp32 logits takes 5.9 us without alternatives and 9.0 with 20.
 template <class T, int NT>
-__global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
-                                                      Partial* __restrict__ partial,
-                                                      Key* __restrict__ seg_top) {
-  constexpr int N = Row<T>::N, kWaves = NT / 64, kGroup = NT / 64;
+__global__ void __launch_bounds__(NT)
+logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
+                Partial* __restrict__ partial, Key* __restrict__ seg_top) {
+  constexpr int N = kPerVector<T>, kWaves = NT / 64, kGroup = NT / 64;
+  constexpr int kPicked = kMaxTop * kGroup;        // the keys of kMaxTop groups
+  constexpr int kFound = NT == 64 ? 512 : 1024;    // elements kept before the slow selection
   __shared__ double sd[2][kWaves];
   __shared__ float sf[kWaves];
-  __shared__ Key group_key[64], picked[kPicked], chosen[kMaxTop], found[kFound];
+  __shared__ Key group_key[64], picked[kPicked], found[kFound], tighter;
   __shared__ int npicked, nfound;
-  const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = blockIdx.y;
   const int64_t t = blockIdx.x;
-  const int seg = int(blockIdx.y);
   const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
-  const int64_t begin = row.vectors * seg / segs, end = row.vectors * (seg + 1) / segs;
+  const int64_t tok = a.tokens ? a.tokens[t] : -1;
+  const uint32_t begin = std::min(seg * seg_vectors, row.vectors);
+  const uint32_t end = std::min(begin + seg_vectors, row.vectors);
   Sums s;
-  auto one = [&](int64_t i) {
-    const float x = T::widen(row.x[i]);
-    s.raise(x);
-    s.add(x);
-    s.note(x, uint32_t(i));
-  };
-  int64_t i = begin + tid;
-  for (; i + (kUnroll - 1) * NT < end; i += kUnroll * NT) {
+#pragma unroll 1
+  for (uint32_t i = begin; i < end; i += kUnroll * NT) {
     uint32x4 v[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) v[u] = row.load(i + u * NT);
+    for (int u = 0; u < kUnroll; ++u) {
+      v[u] = minus_infinity<T>();   // adds nothing
+      if (i + u * NT + tid < end) v[u] = row.load(i + u * NT + tid);
+    }
     float f[kUnroll][N], top = -kInf;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       widen<T>(v[u], f[u]);
       const float l = largest(f[u]);
-      s.note(l, uint32_t((i + u * NT) * N));
+      s.note(l, (i + u * NT + tid) * N);
       top = fmaxf(top, l);
     }
     s.raise(top);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
+      if (i + u * NT < end)
 #pragma unroll
-      for (int k = 0; k < N; ++k) s.add(f[u][k]);
+        for (int k = 0; k < N; ++k) s.add(f[u][k]);
   }
-  for (; i < end; i += NT) {
-    float f[N];
-    widen<T>(row.load(i), f);
-    const float l = largest(f);
-    s.note(l, uint32_t(i * N));
-    s.raise(l);
-#pragma unroll
-    for (int k = 0; k < N; ++k) s.add(f[k]);
+  const uint32_t after = row.vectors * N;
+  const bool has_tail = seg == segs - 1 && tid < row.tail;   // elements after the last vector
+  if (has_tail) {
+    const float x = T::widen(row.x[after + tid]);
+    s.raise(x);
+    s.add(x);
+    s.note(x, after + tid);
   }
-  if (seg == segs - 1 && tid < row.tail) one(a.vocab - row.tail + tid);
+  const Key mine = s.best > -kInf ? order_key(s.best, s.base) : 0;
 
+  const float xtok = segs == 1 ? token_logit<T>(a, t, tok) : 0.f;
   // the sums of the threads
   float m = lanes_reduce(s.m, [](float p, float q) { return fmaxf(p, q); });
   if (lane == 0) sf[wave] = m;
@@ -209,7 +223,6 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
     sd[1][wave] = E;
   }
   // the largest element of each of 64 groups of threads
-  const Key mine = s.best > -kInf ? order_key(s.best, s.base) : 0;
   const Key g = lanes_reduce<kGroup>(mine, max_key);
   if (tid % kGroup == 0) group_key[tid / kGroup] = g;
   __syncthreads();
@@ -218,80 +231,83 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(LogprobArgs a, int segs,
     S += sd[0][w];
     E += sd[1][w];
   }
-  double log_s = 0.0;
-  const int64_t part = t * segs + seg;
-  if (segs > 1) {
-    if (tid == 0) partial[part] = Partial{S, E, m, 0.f};
-  } else {
-    if (tid == 0) write_sums<T>(a, t, m, S, E, log_s);
-    else if (a.top) log_s = S == 0.0 ? -double(kInf) : log(S);
+  const double log_s = log_of(S);
+  const int64_t at = t * int64_t(segs) + seg;
+  if (tid == 0) {
+    if (segs > 1) partial[at] = Partial{S, E, m, 0.f};
+    else write_sums(a, t, tok, xtok, m, S, E, log_s);
   }
   if (a.top == 0) return;
   auto put = [&](int rank, Key key) {
-    if (segs > 1) seg_top[part * a.top + rank] = key;
+    if (segs > 1) seg_top[at * a.top + rank] = key;
     else write_alternative(a, t, rank, key, m, log_s);
   };
   if (!(S > 0.0)) {   // nothing left, or no distribution (the same for all threads)
-    for (int k = tid; k < a.top; k += NT) put(k, 0);
+    for (int k = int(tid); k < a.top; k += NT) put(k, 0);
     return;
   }
-  {   // bound over the groups: every wave for itself
+  Key bound;
+  {   // every wave for itself
     const Key key = group_key[lane];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < 64; ++j) rank += group_key[j] > key ? 1 : 0;
-    const unsigned long long at = __ballot(rank == a.top - 1);
-    const Key bound = at ? __shfl(key, __builtin_ctzll(at), 64) : 0;
-    if (mine && mine >= bound) picked[atomicAdd(&npicked, 1)] = mine;
+    const unsigned long long cut = __ballot(rank == a.top - 1);
+    bound = cut ? max_key(__shfl(key, __builtin_ctzll(cut), 64), 1) : 1;   // fewer groups: all keys
+    if (mine >= bound) picked[atomicAdd(&npicked, 1)] = mine;
   }
   __syncthreads();
-  const int nchosen = std::min(npicked, a.top);
-  by_rank(picked, npicked, a.top, [&](int rank, Key key) { chosen[rank] = key; });
-  __syncthreads();
-  const Key bound = npicked < a.top ? 1 : chosen[a.top - 1];
-  auto take = [&](float x, int64_t index, int64_t base) {
-    if (x > -kInf && order_key(x, uint32_t(base)) >= bound) {
+  const int npick = npicked;
+  if (npick > kManyPicked) {
+    by_rank(picked, npick, a.top, [&](int rank, Key key) {
+      if (rank == a.top - 1) tighter = key;
+    });
+    __syncthreads();
+    bound = tighter;
+  }
+  auto take = [&](float x, uint32_t index, uint32_t base) {
+    if (x > -kInf && order_key(x, base) >= bound) {
       const int k = atomicAdd(&nfound, 1);
-      if (k < kFound) found[k] = order_key(x, uint32_t(index));
+      if (k < kFound) found[k] = order_key(x, index);
     }
   };
-  // all threads over (chosen thread, its vectors and its element after the last)
-  const uint32_t each = uint32_t((end - begin + NT - 1) / NT) + 1;
-  for (uint32_t p = uint32_t(tid); p < uint32_t(nchosen) * each; p += NT) {
-    const uint32_t step = p % each;
-    const int64_t first = key_index(chosen[p / each]), after = row.vectors * N;
-    const int64_t owner = first < after ? (first / N - begin) % NT : first - after;
-    if (step == each - 1) {
-      const int64_t e = after + owner;
-      if (seg == segs - 1 && owner < row.tail) take(T::widen(row.x[e]), e, e);
-      continue;
-    }
-    const int64_t v = begin + owner + int64_t(step) * NT;
-    if (v >= end) continue;
+  // all threads over (picked key, the vectors of its thread)
+  const uint32_t each = (end - begin + NT - 1) / NT;
+#pragma unroll 1
+  for (uint32_t p = tid; p < uint32_t(npick) * each; p += NT) {
+    const uint32_t which = p / each;
+    const Key key = picked[which];
+    const uint32_t e = key_index(key);
+    const uint32_t owner = e < after ? (e / N - begin) % NT : e - after;
+    const uint32_t v = begin + owner + (p - which * each) * NT;
+    if (key < bound || v >= end) continue;
     float f[N];
     widen<T>(row.load(v), f);
-    if (order_key(largest(f), uint32_t(v * N)) >= bound)
+    if (order_key(largest(f), v * N) >= bound)
 #pragma unroll
       for (int k = 0; k < N; ++k) take(f[k], v * N + k, v * N);
   }
+  if (has_tail) take(T::widen(row.x[after + tid]), after + tid, after + tid);
   __syncthreads();
   const int n = nfound;
   if (n <= kFound) {
     by_rank(found, n, a.top, put);
-    for (int k = n + tid; k < a.top; k += NT) put(k, 0);
+    for (int k = n + int(tid); k < a.top; k += NT) put(k, 0);
     return;
   }
   // More elements reach the bound than are kept, as when a thread's elements are all
   // among the largest: one pass over the segment for each alternative.
   Key last = ~Key(0);
+  const uint32_t stop = seg == segs - 1 ? uint32_t(a.vocab) : end * N;
+#pragma unroll 1
   for (int k = 0; k < a.top; ++k) {
     Key best = 0;
-    auto look = [&](int64_t e) {
+#pragma unroll 1
+    for (uint32_t e = begin * N + tid; e < stop; e += NT) {
       const float x = T::widen(row.x[e]);
-      const Key key = order_key(x, uint32_t(e));
+      const Key key = order_key(x, e);
       if (x > -kInf && key < last && key > best) best = key;
-    };
-    for (int64_t e = begin * N + tid; e < end * N; e += NT) look(e);
-    if (seg == segs - 1 && tid < row.tail) look(a.vocab - row.tail + tid);
+    }
     best = lanes_reduce(best, max_key);
     __syncthreads();
     if (lane == 0) picked[wave] = best;
@@ -312,6 +328,8 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(LogprobArgs a, int s
   __shared__ int n;
   const int64_t t = blockIdx.x;
   const Partial* part = partial + t * segs;
+  const int64_t tok = a.tokens ? a.tokens[t] : -1;
+  const float xtok = token_logit<T>(a, t, tok);
   float m = part[0].m;
   for (int s = 1; s < segs; ++s) m = fmaxf(m, part[s].m);
   double S = 0, E = 0;
@@ -321,9 +339,9 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(LogprobArgs a, int s
     S += c * part[s].S;
     E += c * (part[s].E + double(d) * part[s].S);
   }
-  double log_s = S == 0.0 ? -double(kInf) : log(S);
+  const double log_s = log_of(S);
   if (threadIdx.x == 0) {
-    write_sums<T>(a, t, m, S, E, log_s);
+    write_sums(a, t, tok, xtok, m, S, E, log_s);
     n = 0;
   }
   if (a.top == 0) return;
@@ -374,9 +392,9 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(Logprob
   const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
   typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
   const GradRow r(a, t);
-  const int tid = int(threadIdx.x);
+  const uint32_t tid = threadIdx.x;
   if (blockIdx.y == 0 && tid < row.tail) {
-    const int64_t e = row.vectors * N + tid;
+    const uint32_t e = row.vectors * N + tid;
     out[e] = T::narrow(r.at(T::widen(row.x[e]), e));
   }
   constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;
@@ -385,7 +403,7 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(Logprob
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t i = b + u * kGradThreads + tid;
-      if (i < row.vectors) v[u] = row.load(i);
+      if (i < row.vectors) v[u] = row.load(uint32_t(i));
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -404,35 +422,43 @@ size_t partial_bytes(int64_t nrows, int segs) {
   return align256(size_t(nrows) * segs * sizeof(Partial));
 }
 
-// Segments of a row.
-int segments(int64_t nrows, int64_t vocab) {
-  if (nrows >= 256) return 1;
-  const int64_t want = std::min<int64_t>(512 / nrows, vocab / 32768);
-  return int(std::max<int64_t>(1, std::min<int64_t>(want, kMaxSegs)));
+// Segments of a row: with few rows, rows of 2^18 bytes and more are cut so that a
+// workgroup has 8 vectors a thread, up to a workgroup for each CU. The join is a second
+// kernel, so shorter rows are left whole: 1 x 64000 fp32 with 20 alternatives takes 12.1
+// us whole and 13.1 in four, 1 x 131072 fp32 with 5 16.6 and 12.7 in eight, 64 x 131072
+// bf16 17.6 and 15.2 in four, 128 x 60000 fp32 13.2 and 16.7 in four.
+int segments(int64_t nrows, int64_t vocab, int per_vector) {
+  const int64_t n = vocab / per_vector;
+  if (n < 16384) return 1;
+  return int(std::max<int64_t>(1, std::min<int64_t>({n / 4096, 256 / nrows, kMaxSegs})));
 }
 
 }  // namespace
 
 size_t token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int top) {
-  const int segs = segments(nrows, vocab);
+  const int segs = segments(nrows, vocab, 4);   // the type with the most
   if (segs == 1) return 0;
   return partial_bytes(nrows, segs) + align256(size_t(nrows) * segs * top * sizeof(Key));
 }
 
 hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void* d_ws, hipStream_t stream) {
-  const int segs = segments(a.nrows, a.vocab);
-  const dim3 grid(unsigned(a.nrows), unsigned(segs));
-  Partial* part = static_cast<Partial*>(d_ws);
-  Key* keys = reinterpret_cast<Key*>(static_cast<char*>(d_ws) + partial_bytes(a.nrows, segs));
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const int64_t per = a.vocab / segs;
-    if (per <= 2048)
-      hipLaunchKernelGGL((logprobs_kernel<T, 64>), grid, dim3(64), 0, stream, a, segs, part, keys);
-    else if (per <= 8192 || a.nrows * segs >= 512)
-      hipLaunchKernelGGL((logprobs_kernel<T, 256>), grid, dim3(256), 0, stream, a, segs, part, keys);
-    else
-      hipLaunchKernelGGL((logprobs_kernel<T, 1024>), grid, dim3(1024), 0, stream, a, segs, part, keys);
+    const int segs = segments(a.nrows, a.vocab, kPerVector<T>);
+    Partial* part = static_cast<Partial*>(d_ws);
+    Key* keys = reinterpret_cast<Key*>(static_cast<char*>(d_ws) + partial_bytes(a.nrows, segs));
+    const uint32_t n = uint32_t(a.vocab) / kPerVector<T>;
+    auto go = [&](auto kern, unsigned threads) {
+      hipLaunchKernelGGL(kern, dim3(unsigned(a.nrows), unsigned(segs)), dim3(threads), 0, stream, a,
+                         uint32_t(segs), (n + segs - 1) / segs, part, keys);
+    };
+    // One wave where a row is short, or rather short and there are many (4096 x 4000 bf16
+    // 15.0 us, with 4 waves 22.1; 700 x 16000 16.6 and 12.1); eight where it is long or
+    // there are few (2048 x 131072 bf16 109 us, with 4 waves 111; 1 x 32000 fp32 9.0 and
+    // 12.1; 4096 x 32000 bf16 66 and 62).
+    if (n <= 256 || (n <= 1024 && a.nrows >= 1024)) go(logprobs_kernel<T, 64>, 64);
+    else if (n < 8192 && a.nrows > 512) go(logprobs_kernel<T, 256>, 256);
+    else go(logprobs_kernel<T, 512>, 512);
     if (segs > 1)
       hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(unsigned(a.nrows)), dim3(256), 0, stream, a,
                          segs, part, keys);
