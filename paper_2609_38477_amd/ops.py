@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 from dataclasses import dataclass
 
 from . import _check, _ptr, _stream
@@ -110,6 +111,14 @@ def seedq_token_logprobs_backward(d_logits, type: int, ld: int, nrows: int, voca
 
 
 # ---------------------------------------------------------------- helpers
+#
+# A call for one token is bound by the way through these lines, so they take the
+# pointers and the stream's handle directly. The workspaces' sizes are functions of the
+# arguments below alone.
+
+_gemv_workspace = functools.lru_cache(maxsize=256)(seedq_q4_gemv_workspace_bytes)
+_logprobs_workspace = functools.lru_cache(maxsize=256)(seedq_token_logprobs_workspace_bytes)
+
 
 def _type(dtype, what: str) -> int:
     """The SEEDQ_* code of a torch dtype."""
@@ -126,11 +135,20 @@ def _type(dtype, what: str) -> int:
 def _on(stream):
     """The stream that a helper allocates and launches on."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _current
     import torch
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(stream)
     return torch.cuda.stream(stream)
+
+
+_current = contextlib.nullcontext()
+
+
+def _handle(device: int) -> int:
+    """Handle of the current stream of a device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _device(t, what: str) -> int:
@@ -141,19 +159,21 @@ def _device(t, what: str) -> int:
     return i
 
 
-def _same(t, like, shape, dtype, what: str) -> None:
-    """t is a dense tensor of this shape and type on like's device."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() \
-            or t.get_device() != like.get_device():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {like.device} "
+def _same(t, device: int, shape, dtype, what: str) -> None:
+    """t is a dense tensor of this shape and type on this device."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {device} "
                          f"wanted, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _rows(t):
-    """t [n, m] with elements of a row side by side and rows that do not overlap."""
+    """t [n, m] with elements of a row side by side and rows that do not overlap, and
+    its row stride."""
     n, m = t.shape
+    if t.is_contiguous():
+        return t, m
     if (m > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < m):
-        t = t.contiguous()
+        return t.contiguous(), m
     return t, (t.stride(0) if n > 1 else m)
 
 
@@ -170,14 +190,17 @@ class Q4Weights:
     group: int
 
 
-def _check_q4(q: Q4Weights) -> None:
+def _check_q4(q: Q4Weights) -> int:
+    """The device of q, whose tensors are what its sizes say."""
     import torch
-    _device(q.codes, "codes")
-    _same(q.codes, q.codes, (q.nrows, 4 * ((q.ncols + 31) // 32)), torch.int32, "codes")
+    codes, zero = q.codes, q.zero
+    device = _device(codes, "codes")
     groups = (q.nrows, -(-q.ncols // q.group))
-    _same(q.scale, q.codes, groups, torch.float16, "scale")
-    if q.zero is not None:
-        _same(q.zero, q.codes, groups, torch.uint8, "zero")
+    _same(codes, device, (q.nrows, 4 * ((q.ncols + 31) // 32)), torch.int32, "codes")
+    _same(q.scale, device, groups, torch.float16, "scale")
+    if zero is not None:
+        _same(zero, device, groups, torch.uint8, "zero")
+    return device
 
 
 def q4_quantize(W, group: int = 128, zeros: bool = False, stream=None) -> Q4Weights:
@@ -190,15 +213,17 @@ def q4_quantize(W, group: int = 128, zeros: bool = False, stream=None) -> Q4Weig
         raise ValueError(f"W: two dimensions wanted, not {W.dim()}")
     if group not in GROUPS:
         raise ValueError(f"group: one of {GROUPS} wanted, not {group}")
-    _device(W, "W")
+    device = _device(W, "W")
     nrows, ncols = W.shape
+    groups = (nrows, -(-ncols // group))
     with _on(stream):
         W, ldw = _rows(W)
-        codes = torch.empty((nrows, 4 * ((ncols + 31) // 32)), dtype=torch.int32, device=W.device)
-        groups = (nrows, -(-ncols // group))
-        scale = torch.empty(groups, dtype=torch.float16, device=W.device)
-        zero = torch.empty(groups, dtype=torch.uint8, device=W.device) if zeros else None
-        seedq_q4_quantize(W, t, ldw, nrows, ncols, group, codes, scale, zero)
+        codes = W.new_empty((nrows, 4 * ((ncols + 31) // 32)), dtype=torch.int32)
+        scale = W.new_empty(groups, dtype=torch.float16)
+        zero = W.new_empty(groups, dtype=torch.uint8) if zeros else None
+        _check(lib().seedq_q4_quantize(W.data_ptr(), t, ldw, nrows, ncols, group, codes.data_ptr(),
+                                       scale.data_ptr(), _ptr(zero), _handle(device)),
+               "seedq_q4_quantize")
     return Q4Weights(codes, scale, zero, nrows, ncols, group)
 
 
@@ -207,10 +232,13 @@ def q4_dequantize(q: Q4Weights, dtype=None, stream=None):
     import torch
     dtype = torch.float32 if dtype is None else dtype
     t = _type(dtype, "dtype")
-    _check_q4(q)
+    device = _check_q4(q)
+    nrows, ncols = q.nrows, q.ncols
     with _on(stream):
-        W = torch.empty((q.nrows, q.ncols), dtype=dtype, device=q.codes.device)
-        seedq_q4_dequantize(q.codes, q.scale, q.zero, q.nrows, q.ncols, q.group, W, t, q.ncols)
+        W = q.codes.new_empty((nrows, ncols), dtype=dtype)
+        _check(lib().seedq_q4_dequantize(q.codes.data_ptr(), q.scale.data_ptr(), _ptr(q.zero), nrows,
+                                         ncols, q.group, W.data_ptr(), t, ncols, _handle(device)),
+               "seedq_q4_dequantize")
     return W
 
 
@@ -223,20 +251,23 @@ def q4_gemv(q: Q4Weights, x, out_dtype=None, stream=None):
     yt = _type(out_dtype, "out_dtype")
     if yt != xt and yt != SEEDQ_F32:
         raise TypeError(f"out_dtype: {x.dtype} or float32 wanted, not {out_dtype}")
-    if x.dim() not in (1, 2) or x.shape[-1] != q.ncols:
-        raise ValueError(f"x: [{q.ncols}] or [nvec, {q.ncols}] wanted, not {tuple(x.shape)}")
-    _check_q4(q)
-    if x.get_device() != q.codes.get_device():
+    nrows, ncols = q.nrows, q.ncols
+    single = x.dim() == 1
+    if x.dim() not in (1, 2) or x.shape[-1] != ncols:
+        raise ValueError(f"x: [{ncols}] or [nvec, {ncols}] wanted, not {tuple(x.shape)}")
+    device = _check_q4(q)
+    if x.get_device() != device:
         raise ValueError(f"x: on {x.device}, the codes on {q.codes.device}")
     with _on(stream):
-        xx, ldx = _rows(x if x.dim() == 2 else x.unsqueeze(0))
+        xx, ldx = _rows(x.unsqueeze(0) if single else x)
         nvec = xx.shape[0]
-        y = torch.empty((nvec, q.nrows), dtype=out_dtype, device=x.device)
-        nws = seedq_q4_gemv_workspace_bytes(q.nrows, q.ncols, nvec, xt)
-        ws = torch.empty(nws, dtype=torch.uint8, device=x.device) if nws else None
-        seedq_q4_gemv(q.codes, q.scale, q.zero, q.nrows, q.ncols, q.group, nvec, xx, xt, ldx, y, yt,
-                      q.nrows, ws, nws)
-    return y if x.dim() == 2 else y[0]
+        y = xx.new_empty((nvec, nrows), dtype=out_dtype)
+        nws = _gemv_workspace(nrows, ncols, nvec, xt)
+        ws = xx.new_empty(nws, dtype=torch.uint8) if nws else None
+        _check(lib().seedq_q4_gemv(q.codes.data_ptr(), q.scale.data_ptr(), _ptr(q.zero), nrows, ncols,
+                                   q.group, nvec, xx.data_ptr(), xt, ldx, y.data_ptr(), yt, nrows,
+                                   _ptr(ws), nws, _handle(device)), "seedq_q4_gemv")
+    return y[0] if single else y
 
 
 @dataclass
@@ -250,11 +281,11 @@ class TokenLogprobs:
 
 
 def _logits(logits, what: str):
+    """Type code and device of rows of logits."""
     t = _type(logits.dtype, what)
     if logits.dim() != 2 or logits.shape[1] < 1:
         raise ValueError(f"{what}: [nrows, vocab] wanted, not {tuple(logits.shape)}")
-    _device(logits, what)
-    return t
+    return t, _device(logits, what)
 
 
 def token_logprobs(logits, tokens=None, top: int = 0, stream=None) -> TokenLogprobs:
@@ -263,24 +294,26 @@ def token_logprobs(logits, tokens=None, top: int = 0, stream=None) -> TokenLogpr
     nothing and gives 0), the entropy, the log of the sum, and the ``top`` likeliest
     tokens with their log probabilities."""
     import torch
-    t = _logits(logits, "logits")
+    t, device = _logits(logits, "logits")
     nrows, vocab = logits.shape
     if not 0 <= top <= SEEDQ_MAX_TOP:
         raise ValueError(f"top: 0 to {SEEDQ_MAX_TOP} wanted, not {top}")
     if tokens is not None:
-        _same(tokens, logits, (nrows,), torch.int64, "tokens")
+        _same(tokens, device, (nrows,), torch.int64, "tokens")
     with _on(stream):
         x, ld = _rows(logits)
-        dev = x.device
-        sums = torch.empty((3, nrows), dtype=torch.float32, device=dev)
+        sums = x.new_empty((3, nrows), dtype=torch.float32)
         lse, entropy, logprob = sums.unbind(0)
-        logprob = None if tokens is None else logprob
-        top_token = torch.empty((nrows, top), dtype=torch.int64, device=dev) if top else None
-        top_logprob = torch.empty((nrows, top), dtype=torch.float32, device=dev) if top else None
-        nws = seedq_token_logprobs_workspace_bytes(nrows, vocab, top)
-        ws = torch.empty(nws, dtype=torch.uint8, device=dev) if nws else None
-        seedq_token_logprobs(x, t, ld, nrows, vocab, tokens, top, logprob, entropy, lse, top_token,
-                             top_logprob, ws, nws)
+        if tokens is None:
+            logprob = None
+        top_token = x.new_empty((nrows, top), dtype=torch.int64) if top else None
+        top_logprob = x.new_empty((nrows, top), dtype=torch.float32) if top else None
+        nws = _logprobs_workspace(nrows, vocab, top)
+        ws = x.new_empty(nws, dtype=torch.uint8) if nws else None
+        _check(lib().seedq_token_logprobs(x.data_ptr(), t, ld, nrows, vocab, _ptr(tokens), top,
+                                          _ptr(logprob), entropy.data_ptr(), lse.data_ptr(),
+                                          _ptr(top_token), _ptr(top_logprob), _ptr(ws), nws,
+                                          _handle(device)), "seedq_token_logprobs")
     return TokenLogprobs(logprob, entropy, lse, top_token, top_logprob)
 
 
@@ -290,7 +323,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None
     entropy_t), from what token_logprobs gave; either gradient may be None. ``out``
     (the logits' type and shape) may be the logits themselves."""
     import torch
-    t = _logits(logits, "logits")
+    t, device = _logits(logits, "logits")
     nrows, vocab = logits.shape
     if grad_logprob is None and grad_entropy is None:
         raise ValueError("grad_logprob or grad_entropy wanted")
@@ -299,18 +332,23 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None
     if grad_entropy is not None and entropy is None:
         raise ValueError("grad_entropy needs entropy")
     if tokens is not None:
-        _same(tokens, logits, (nrows,), torch.int64, "tokens")
+        _same(tokens, device, (nrows,), torch.int64, "tokens")
     for name, v in (("lse", lse), ("entropy", entropy), ("grad_logprob", grad_logprob),
                     ("grad_entropy", grad_entropy)):
         if v is not None:
-            _same(v, logits, (nrows,), torch.float32, name)
+            _same(v, device, (nrows,), torch.float32, name)
     with _on(stream):
         x, ld = _rows(logits)
         if out is None:
-            out = torch.empty((nrows, vocab), dtype=x.dtype, device=x.device)
-        elif out.dtype != x.dtype or out.shape != x.shape or out.get_device() != x.get_device() \
+            out, ldg = x.new_empty((nrows, vocab)), vocab
+        elif out.dtype != x.dtype or out.shape != x.shape or out.get_device() != device \
                 or (vocab > 1 and out.stride(1) != 1) or (nrows > 1 and out.stride(0) < vocab):
             raise ValueError("out: the logits' type, shape and device, with dense rows, wanted")
-        seedq_token_logprobs_backward(x, t, ld, nrows, vocab, tokens, lse, entropy, grad_logprob,
-                                      grad_entropy, out, out.stride(0) if nrows > 1 else ld)
+        else:
+            ldg = out.stride(0) if nrows > 1 else ld
+        _check(lib().seedq_token_logprobs_backward(x.data_ptr(), t, ld, nrows, vocab, _ptr(tokens),
+                                                   lse.data_ptr(), _ptr(entropy), _ptr(grad_logprob),
+                                                   _ptr(grad_entropy), out.data_ptr(), ldg,
+                                                   _handle(device)),
+               "seedq_token_logprobs_backward")
     return out
