@@ -441,9 +441,24 @@ size_t token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int top) {
   return partial_bytes(nrows, segs) + align256(size_t(nrows) * segs * top * sizeof(Key));
 }
 
-hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void* d_ws, hipStream_t stream) {
+hipError_t launch_token_logprobs(const LogprobArgs& all, int type, void* d_ws, hipStream_t stream) {
+  if (all.nrows > kMaxRows) {   // never in segments
+    for (int64_t r = 0; r < all.nrows; r += kMaxRows) {
+      const auto from = [&](auto* p, int64_t each) { return p ? p + r * each : p; };
+      LogprobArgs a = all;
+      a.logits = static_cast<const char*>(all.logits) + r * all.ld * (type == SEEDQ_F32 ? 4 : 2);
+      a.nrows = std::min(kMaxRows, all.nrows - r);
+      a.tokens = from(all.tokens, 1);
+      a.logprob = from(all.logprob, 1), a.entropy = from(all.entropy, 1), a.lse = from(all.lse, 1);
+      a.top_token = from(all.top_token, all.top), a.top_logprob = from(all.top_logprob, all.top);
+      const hipError_t e = launch_token_logprobs(a, type, d_ws, stream);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
   return with_type(type, [&](auto t) {
     using T = decltype(t);
+    const LogprobArgs& a = all;
     const int segs = segments(a.nrows, a.vocab, kPerVector<T>);
     Partial* part = static_cast<Partial*>(d_ws);
     Key* keys = reinterpret_cast<Key*>(static_cast<char*>(d_ws) + partial_bytes(a.nrows, segs));
@@ -466,9 +481,25 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, int type, void* d_ws, hip
   });
 }
 
-hipError_t launch_token_logprobs_backward(const LogprobGradArgs& a, int type, hipStream_t stream) {
+hipError_t launch_token_logprobs_backward(const LogprobGradArgs& all, int type, hipStream_t stream) {
+  if (all.nrows > kMaxRows) {
+    for (int64_t r = 0; r < all.nrows; r += kMaxRows) {
+      const auto from = [&](auto* p) { return p ? p + r : p; };
+      const int64_t size = type == SEEDQ_F32 ? 4 : 2;
+      LogprobGradArgs a = all;
+      a.logits = static_cast<const char*>(all.logits) + r * all.ld * size;
+      a.grad = static_cast<char*>(all.grad) + r * all.ldg * size;
+      a.nrows = std::min(kMaxRows, all.nrows - r);
+      a.tokens = from(all.tokens);
+      a.lse = from(all.lse), a.entropy = from(all.entropy), a.g = from(all.g), a.h = from(all.h);
+      const hipError_t e = launch_token_logprobs_backward(a, type, stream);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
   return with_type(type, [&](auto t) {
     using T = decltype(t);
+    const LogprobGradArgs& a = all;
     const int64_t step = int64_t(kUnroll) * kGradThreads * kPerVector<T>;
     const dim3 grid(unsigned(a.nrows),
                     unsigned(std::min<int64_t>((a.vocab + step - 1) / step, 65535)));

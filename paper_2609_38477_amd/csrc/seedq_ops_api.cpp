@@ -55,9 +55,7 @@ int seedq_q4_quantize(const void* d_W, int32_t type, int64_t ldw, int64_t nrows,
   const int rc = q4_args(d_codes, d_scale, d_zero, nrows, ncols, group, q);
   if (rc != SEEDQ_OK) return rc;
   if (!d_W || misaligned(d_W, type_size(type)) || !ld_ok(ldw, ncols)) return SEEDQ_EINVAL;
-  return result(launch_q4_quantize(d_W, type, ldw, nrows, ncols, q.gshift, d_codes,
-                                   static_cast<uint16_t*>(d_scale), d_zero,
-                                   static_cast<hipStream_t>(hip_stream)));
+  return result(launch_q4_quantize(d_W, type, ldw, q, static_cast<hipStream_t>(hip_stream)));
 }
 
 int seedq_q4_dequantize(const uint32_t* d_codes, const void* d_scale, const uint8_t* d_zero,

@@ -9,6 +9,9 @@ namespace seedq {
 inline int64_t q4_row_words(int64_t ncols) { return 4 * ((ncols + 31) / 32); }
 inline int64_t q4_groups(int64_t ncols, int group) { return (ncols + group - 1) / group; }
 
+// Rows of one launch: a grid has fewer than 2^32 threads along a dimension.
+constexpr int64_t kMaxRows = int64_t(1) << 21;
+
 // A matrix in 4 bits. gshift = log2(group); zero may be null.
 struct Q4 {
   const uint32_t* codes;
@@ -16,10 +19,19 @@ struct Q4 {
   const uint8_t* zero;
   int64_t nrows, ncols, row_words, ngroups;
   int gshift;
+  // Up to kMaxRows rows from row r on.
+  Q4 rows(int64_t r) const {
+    Q4 q = *this;
+    q.codes += r * row_words;
+    q.scale += r * ngroups;
+    if (zero) q.zero += r * ngroups;
+    q.nrows = nrows - r < kMaxRows ? nrows - r : kMaxRows;
+    return q;
+  }
 };
 
-hipError_t launch_q4_quantize(const void* d_W, int type, int64_t ldw, int64_t nrows, int64_t ncols,
-                              int gshift, uint32_t* d_codes, uint16_t* d_scale, uint8_t* d_zero,
+// q's arrays are written.
+hipError_t launch_q4_quantize(const void* d_W, int type, int64_t ldw, const Q4& q,
                               hipStream_t stream);
 hipError_t launch_q4_dequantize(const Q4& q, void* d_W_hat, int type, int64_t ldw,
                                 hipStream_t stream);

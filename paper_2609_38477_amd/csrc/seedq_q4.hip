@@ -24,10 +24,13 @@ __device__ __forceinline__ float rounded_quotient(float w, float s, float inv) {
 
 template <class T, bool ZEROS>
 __global__ void __launch_bounds__(kThreads)
-quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, int64_t nrows, int64_t ncols,
-                int64_t row_words, int64_t ngroups, int gshift, uint32_t tiles, int64_t total,
-                uint32_t* __restrict__ codes, uint16_t* __restrict__ scale,
-                uint8_t* __restrict__ zero) {
+quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, Q4 q, uint32_t tiles,
+                int64_t total) {
+  uint32_t* __restrict__ codes = const_cast<uint32_t*>(q.codes);
+  uint16_t* __restrict__ scale = const_cast<uint16_t*>(q.scale);
+  uint8_t* __restrict__ zero = const_cast<uint8_t*>(q.zero);
+  const int64_t ncols = q.ncols;
+  const int gshift = q.gshift;
   const int lane = int(threadIdx.x & 63);
   const int64_t job = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
   if (job >= total) return;
@@ -68,9 +71,9 @@ quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, int64_t nrow
       code |= uint32_t(fminf(fmaxf(t + z, 0.f), 15.f)) << (4 * i);
     }
   }
-  if (word < row_words) codes[r * row_words + word] = code;   // zero after the last column
+  if (word < q.row_words) codes[r * q.row_words + word] = code;   // zero after the last column
   if (c < ncols && (lane & (lanes - 1)) == 0) {
-    const int64_t g = r * ngroups + (c >> gshift);
+    const int64_t g = r * q.ngroups + (c >> gshift);
     scale[g] = finite ? __builtin_bit_cast(uint16_t, sh) : uint16_t(0x7E00);
     if (ZEROS) zero[g] = finite ? uint8_t(z) : uint8_t(0);
   }
@@ -112,32 +115,35 @@ Jobs jobs(int64_t nrows, int64_t words) {
 
 }  // namespace
 
-hipError_t launch_q4_quantize(const void* d_W, int type, int64_t ldw, int64_t nrows, int64_t ncols,
-                              int gshift, uint32_t* d_codes, uint16_t* d_scale, uint8_t* d_zero,
+hipError_t launch_q4_quantize(const void* d_W, int type, int64_t ldw, const Q4& q,
                               hipStream_t stream) {
-  const int64_t row_words = q4_row_words(ncols), ngroups = q4_groups(ncols, 1 << gshift);
-  const Jobs j = jobs(nrows, row_words);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     using raw = typename T::raw;
-    auto launch = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3(j.grid), dim3(kThreads), 0, stream, static_cast<const raw*>(d_W),
-                         ldw, nrows, ncols, row_words, ngroups, gshift, j.tiles, j.total, d_codes,
-                         d_scale, d_zero);
-    };
-    d_zero ? launch(quantize_kernel<T, true>) : launch(quantize_kernel<T, false>);
+    for (int64_t r = 0; r < q.nrows; r += kMaxRows) {
+      const Q4 part = q.rows(r);
+      const Jobs j = jobs(part.nrows, q.row_words);
+      auto launch = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(j.grid), dim3(kThreads), 0, stream,
+                           static_cast<const raw*>(d_W) + r * ldw, ldw, part, j.tiles, j.total);
+      };
+      q.zero ? launch(quantize_kernel<T, true>) : launch(quantize_kernel<T, false>);
+    }
     return hipGetLastError();
   });
 }
 
 hipError_t launch_q4_dequantize(const Q4& q, void* d_W_hat, int type, int64_t ldw,
                                 hipStream_t stream) {
-  const Jobs j = jobs(q.nrows, q.ncols / kC);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     using raw = typename T::raw;
-    hipLaunchKernelGGL(dequantize_kernel<T>, dim3(j.grid), dim3(kThreads), 0, stream, q, j.tiles,
-                       j.total, static_cast<raw*>(d_W_hat), ldw);
+    for (int64_t r = 0; r < q.nrows; r += kMaxRows) {
+      const Q4 part = q.rows(r);
+      const Jobs j = jobs(part.nrows, q.ncols / kC);
+      hipLaunchKernelGGL(dequantize_kernel<T>, dim3(j.grid), dim3(kThreads), 0, stream, part, j.tiles,
+                         j.total, static_cast<raw*>(d_W_hat) + r * ldw, ldw);
+    }
     return hipGetLastError();
   });
 }
