@@ -116,151 +116,183 @@ __device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v)
 
 // ---------------------------------------------------------------- few vectors
 
-// One or two vectors, on the vector ALU. A wave holds a slab of columns of x in
-// registers, WORDS words of codes a lane, and goes over kRows rows whose codes it reads
-// at once; a lane's columns lie in one group, so the scale enters once a lane and row.
-// The products u - z (fp16) times x (widened to fp32) are fused multiply-adds that read
-// either half of a register. Order of the sums: the columns of a lane, the slabs of a
-// wave, the lanes as a tree, the waves one after the other.
-constexpr int kRows = 8;
+// One or two vectors, or up to four in fp32, on the vector ALU. The vectors lie in LDS (a panel of kPanelBytes
+// of them, which is all of them but for very long rows) and the waves go over the rows: RB
+// rows a wave at a time, 2048 columns of them a step, 16 bytes of codes a lane, the next
+// steps' codes on their way. A lane's columns lie in one group, so the scale enters once a
+// lane and step. The products u - z (fp16) times x are fused multiply-adds in fp32 that read
+// either half of a register. Where rows are few, `slices` waves share them, each with
+// steps of its own. Order of the sums: the columns of a lane and step, the steps, the
+// lanes as a tree, the slices in order.
 constexpr int kMaxWaves = 16;
+constexpr int kStepCols = 64 * 4 * kC;
+constexpr int kPanelBytes = 128 << 10;
 
-template <class X, int NV, int WORDS>
+template <class X>
+struct FewX {   // 8 columns of x as they lie in LDS
+  static constexpr int kPlanes = sizeof(typename X::raw) == 4 ? 2 : 1;
+  uint32x4 v[kPlanes];
+};
+
+template <class X, int NV, int RB>
 __global__ void __launch_bounds__(64 * kMaxWaves)
-gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int slabs,
+gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int panel_steps, int slices,
                 void* __restrict__ y, int ytype, int64_t ldy) {
-  __shared__ float part[kMaxWaves][NV][kRows];
-  const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), waves = int(blockDim.x >> 6);
-  const int64_t r0 = int64_t(blockIdx.x) * kRows;
-  float acc[NV][kRows] = {};
-  for (int slab = wave; slab < slabs; slab += waves) {
-    const int64_t w0 = (int64_t(slab) * 64 + lane) * WORDS;
-    const int64_t wl = w0 * kC < q.ncols ? w0 : 0;   // idle lanes: the row's start, x as zeros
-    const int64_t g = wl * kC >> q.gshift;
-    uint32_t code[kRows][WORDS];
-    float s[kRows], z[kRows];
+  constexpr int kPlanes = FewX<X>::kPlanes;
+  extern __shared__ uint32x4 panel[];   // [step][plane][vector][4][64]
+  __shared__ float part[kMaxWaves][NV][RB];
+  const int lane = int(threadIdx.x & 63);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
+  const int slots = int(blockDim.x >> 6) / slices, slot = wave / slices, slice = wave % slices;
+  const int steps = int((q.ncols + kStepCols - 1) / kStepCols);
+  const int64_t batches = (q.nrows + RB - 1) / RB;
+  for (int64_t b0 = int64_t(blockIdx.x) * slots; b0 < batches; b0 += int64_t(gridDim.x) * slots) {
+    const int64_t r0 = (b0 + slot) * RB;
+    const bool some = r0 < q.nrows;
+    const uint32_t* crow[RB];
+    int64_t grow[RB];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < RB; ++i) {
       const int64_t r = std::min(r0 + i, q.nrows - 1);
-      const uint32_t* p = q.codes + r * q.row_words + wl;
-      if constexpr (WORDS == 4) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        code[i][0] = v.x, code[i][1] = v.y, code[i][2] = v.z, code[i][3] = v.w;
-      } else if constexpr (WORDS == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        code[i][0] = v.x, code[i][1] = v.y;
-      } else {
-        code[i][0] = *p;
-      }
-      s[i] = F16::widen(q.scale[r * q.ngroups + g]);
-      z[i] = q.zero ? float(q.zero[r * q.ngroups + g] & 15) : 8.f;
+      crow[i] = q.codes + r * q.row_words;
+      grow[i] = r * q.ngroups;
     }
-    float xf[NV][WORDS][8];
+    struct Codes {
+      uint32x4 code[RB];
+      uint16_t s[RB];
+      uint8_t z[RB];
+    };
+    auto fetch = [&](Codes& c, int step) __attribute__((always_inline)) {
+      const int64_t w = int64_t(step) * 256 + lane * 4;
+      const int64_t wl = w * kC < q.ncols ? w : 0;   // idle lanes: the row's start, x is zero there
+      const int64_t g = wl * kC >> q.gshift;
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        c.code[i] = *reinterpret_cast<const uint32x4*>(crow[i] + wl);
+        c.s[i] = q.scale[grow[i] + g];
+        c.z[i] = q.zero ? q.zero[grow[i] + g] & 15 : 8;
+      }
+    };
+    float acc[NV][RB] = {};
+    for (int p0 = 0; p0 < steps; p0 += panel_steps) {
+      const int p1 = std::min(p0 + panel_steps, steps), n = p1 - p0;
+      const int from = p0 + n * slice / slices, to = p0 + n * (slice + 1) / slices;
+      Codes c0, c1;
+      if (some && from < to) fetch(c0, from);
+      if (some && from + 1 < to) fetch(c1, from + 1);
+      if (steps > panel_steps || b0 == int64_t(blockIdx.x) * slots) {
+        __syncthreads();   // the panel before is done with
+        for (int i = int(threadIdx.x); i < n * 256 * NV; i += int(blockDim.x)) {
+          const int v = i / (n * 256), w = i % (n * 256);   // word w of the panel
+          const int64_t c = (int64_t(p0) * 256 + w) * kC;
+          const int at = (w >> 8) * kPlanes * NV * 256 + v * 256 + (w & 3) * 64 + ((w & 255) >> 2);
+#pragma unroll
+          for (int k = 0; k < kPlanes; ++k) {
+            uint32x4 d = {0u, 0u, 0u, 0u};
+            if (c < q.ncols) d = load16(x + v * ldx + c + k * 4);
+            panel[at + k * NV * 256] = d;
+          }
+        }
+        __syncthreads();
+      }
+      if (!some) continue;
+      for (int step = from; step < to; ++step) {
+        Codes c2 = c1;
+        if (step + 2 < to) fetch(c2, step + 2);
+        float d[NV][RB] = {};
+        f16x2 zz[RB];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) zz[i] = f16x2{_Float16(float(c0.z[i])), _Float16(float(c0.z[i]))};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float f[NV][8];
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int k = 0; k < kPlanes; ++k)
+              widen<X>(panel[(((step - p0) * kPlanes + k) * NV + v) * 256 + w * 64 + lane], f[v] + 4 * k);
+#pragma unroll
+          for (int i = 0; i < RB; ++i) {
+            const uint32x4 u = centred(decode<Half>(c0.code[i][w]), zz[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t bits = u[j];
+              const f16x2 pair = __builtin_bit_cast(f16x2, bits);
+#pragma unroll
+              for (int v = 0; v < NV; ++v) {
+                d[v][i] = fmaf(float(pair[0]), f[v][kOrder[2 * j]], d[v][i]);
+                d[v][i] = fmaf(float(pair[1]), f[v][kOrder[2 * j + 1]], d[v][i]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < RB; ++i) acc[v][i] = fmaf(F16::widen(c0.s[i]), d[v][i], acc[v][i]);
+        c0 = c1;
+        c1 = c2;
+      }
+    }
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) {
-        const int64_t c = (w0 + w) * kC;
-        const typename X::raw* xv = x + v * ldx + c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) xf[v][w][i] = 0.f;
-        if (c < q.ncols) load8<X>(xv, xf[v][w]);
-      }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      float d[NV] = {};
-      const f16x2 zz = {_Float16(z[i]), _Float16(z[i])};
-#pragma unroll
-      for (int w = 0; w < WORDS; ++w) {
-        const uint32x4 u = centred(decode<Half>(code[i][w]), zz);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t bits = u[j];
-          const f16x2 pair = __builtin_bit_cast(f16x2, bits);
-#pragma unroll
-          for (int v = 0; v < NV; ++v) {
-            d[v] = fmaf(float(pair[0]), xf[v][w][kOrder[2 * j]], d[v]);
-            d[v] = fmaf(float(pair[1]), xf[v][w][kOrder[2 * j + 1]], d[v]);
-          }
+      for (int i = 0; i < RB; ++i) {
+        acc[v][i] = lanes_reduce(acc[v][i], [](float a, float b) { return a + b; });
+        if (slices > 1) {
+          if (lane == 0) part[wave][v][i] = acc[v][i];
+        } else if (lane == 0 && r0 + i < q.nrows) {
+          store_y(y, ytype, v * ldy + r0 + i, acc[v][i]);
         }
       }
-#pragma unroll
-      for (int v = 0; v < NV; ++v) acc[v][i] = fmaf(s[i], d[v], acc[v][i]);
-    }
-  }
-  // the eight rows' sums over the lanes: halves of the rows change sides with halves of
-  // the lanes, so that lane l ends with row l / 8
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-#pragma unroll
-    for (int n = kRows / 2, d = 32; n >= 1; n >>= 1, d >>= 1) {
-      const bool up = (lane & d) != 0;
-#pragma unroll
-      for (int k = 0; k < n; ++k) {
-        const float keep = up ? acc[v][k + n] : acc[v][k], give = up ? acc[v][k] : acc[v][k + n];
-        acc[v][k] = keep + __shfl_xor(give, d, 64);
+    if (slices > 1) {
+      __syncthreads();
+      for (int k = int(threadIdx.x); k < slots * NV * RB; k += int(blockDim.x)) {
+        const int i = k % RB, sl = k / RB % slots, v = k / RB / slots;
+        float total = part[sl * slices][v][i];
+        for (int s = 1; s < slices; ++s) total += part[sl * slices + s][v][i];
+        const int64_t r = (b0 + sl) * RB + i;
+        if (r < q.nrows) store_y(y, ytype, v * ldy + r, total);
       }
+      __syncthreads();
     }
-    float t = acc[v][0];
-#pragma unroll
-    for (int d = 4; d >= 1; d >>= 1) t += __shfl_xor(t, d, 64);
-    if ((lane & 7) == 0) part[wave][v][lane >> 3] = t;
-  }
-  __syncthreads();
-  for (int k = int(threadIdx.x); k < NV * kRows; k += int(blockDim.x)) {
-    const int v = k / kRows, i = k % kRows;
-    float t = part[0][v][i];
-    for (int w = 1; w < waves; ++w) t += part[w][v][i];
-    if (r0 + i < q.nrows) store_y(y, ytype, v * ldy + r0 + i, t);
   }
 }
 
 // ---------------------------------------------------------------- a batch of vectors
 
-// x in fp32 as three bf16 rows a vector (row 3 v + p), in code order, zeros from ncols
-// to the padded end of the codes' rows.
-__global__ void __launch_bounds__(256)
-split_kernel(const float* __restrict__ x, int64_t ldx, int64_t ncols, int64_t row_words,
-             uint16_t* __restrict__ out) {
-  const int64_t v = blockIdx.y;
-  const int64_t w = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (w >= row_words) return;
-  float f[8] = {};
-  if (w * kC < ncols) load8<F32>(x + v * ldx + w * kC, f);
-  uint32x4 piece[3];
-  split8(f, piece);
-#pragma unroll
-  for (int p = 0; p < 3; ++p)
-    *reinterpret_cast<uint32x4*>(out + ((3 * v + p) * row_words + w) * kC) = piece[p];
-}
-
-// Up to 16 rows of x (vectors, or a third of a vector in fp32) on the matrix core,
-// D = X W^T: a 16x16x32 product takes 16 rows of x and 16 rows of codes. A lane
-// reads 16 bytes of codes of row l % 16, columns 32 (l / 16) .. of a chunk of 128. Where
-// a group is 128 columns or more, product t takes everybody's word t; in smaller groups
-// (NG = 4 or 2 a chunk) the words first change lanes so that product t holds columns
-// 32 t .. 32 t + 31 (four lane swaps). Each group's product and, in bf16, sum of x (a
-// product with ones) meet in fp32 with the scale and zero point of the lane's row. The waves of
-// a workgroup take its chunks in turn and add their sums through LDS in order.
-template <int NG, int RT>
-struct Chunk {
-  uint32x4 code[RT];
-  float s[RT][NG], z[RT][NG];
-  uint32x4 x[4];
+// N neighbouring elements of T at any element.
+template <class T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+  T at[N];
 };
 
-template <class M, int P, int NG, int RT>
-__global__ void __launch_bounds__(64 * kMaxWaves)
-gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx,
-                  void* __restrict__ y, int ytype, int64_t ldy) {
+// Up to 16 vectors of 16 bits on the matrix core, D = X W^T: a 16x16x32 product takes 16 rows of x and 16 rows of codes. A lane
+// reads 16 bytes of codes of row l % 16, columns 32 (l / 16) .. of a chunk of 128. Where
+// a group is 128 columns or more, product t takes everybody's word t; in smaller groups
+// the words first change lanes so that product t holds columns 32 t .. 32 t + 31 (four
+// lane swaps). Each group's product and, in bf16, sum of x (a product with ones) meet in
+// fp32 with the scale and zero point of the lane's row. The waves of a workgroup divide
+// its columns in blocks of BC chunks and add their sums through LDS in order. A block has
+// SB scales a row, which a lane reads at once; its codes are read while the block before
+// is multiplied, x a chunk ahead.
+constexpr int kBatchWaves = 8;
+
+template <class M, int BC, int SB, int RT>
+__global__ void __launch_bounds__(64 * kBatchWaves)
+gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, void* __restrict__ y,
+                  int ytype, int64_t ldy) {
+  constexpr int NG = SB > BC ? SB / BC : 1;          // groups of a chunk
+  constexpr int kSpan = SB < BC ? BC / SB : 1;       // chunks of a group, within the block
   extern __shared__ float part[];
-  const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), waves = int(blockDim.x >> 6);
+  const int lane = int(threadIdx.x & 63), waves = int(blockDim.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int n = lane & 15, kg = lane >> 4;
   const int64_t r0 = int64_t(blockIdx.x) * (16 * RT);
-  const int64_t xcols = P == 3 ? q.row_words * kC : q.ncols;
-  const int64_t chunks = (q.ncols + 127) / 128;
+  const int blocks = int((q.ncols + 128 * BC - 1) / (128 * BC));
+  const int b0 = int(int64_t(blocks) * wave / waves), b1 = int(int64_t(blocks) * (wave + 1) / waves);
   // rows past the last are read as the last and not stored
-  const uint16_t* xrow = x + std::min(n, nvec * P - 1) * ldx;
+  const uint16_t* xrow = x + std::min(n, nvec - 1) * ldx;
   const uint32_t* crow[RT];
   int64_t grow[RT];
 #pragma unroll
@@ -269,63 +301,95 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx,
     crow[t] = q.codes + r * q.row_words;
     grow[t] = r * q.ngroups;
   }
-  auto load = [&](Chunk<NG, RT>& c, int64_t ch) __attribute__((always_inline)) {
+  struct Block {
+    uint32x4 code[RT][BC];
+    Pack<uint16_t, SB> s[RT];
+    Pack<uint8_t, SB> z[RT];
+  };
+  auto load = [&](Block& c, int b) __attribute__((always_inline)) {
+    const int64_t g0 = int64_t(b) * (BC * 128) >> q.gshift;
+    const bool whole = g0 + SB <= q.ngroups;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int64_t w = ch * 16 + kg * 4;
-      c.code[t] = uint32x4{0u, 0u, 0u, 0u};
-      if (w < q.row_words) c.code[t] = *reinterpret_cast<const uint32x4*>(crow[t] + w);
 #pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        const int64_t g = grow[t] + std::min((ch * 128 + j * (128 / NG)) >> q.gshift, q.ngroups - 1);
-        c.s[t][j] = F16::widen(q.scale[g]);
-        c.z[t][j] = q.zero ? float(q.zero[g] & 15) : 8.f;
+      for (int k = 0; k < BC; ++k) {
+        const int64_t w = (int64_t(b) * BC + k) * 16 + kg * 4;
+        c.code[t][k] = uint32x4{0u, 0u, 0u, 0u};
+        if (w < q.row_words) c.code[t][k] = *reinterpret_cast<const uint32x4*>(crow[t] + w);
       }
+      const uint16_t* s = q.scale + grow[t];
+      const uint8_t* z = q.zero + grow[t];
+      if (whole) {
+        c.s[t] = *reinterpret_cast<const Pack<uint16_t, SB>*>(s + g0);
+        if (q.zero) c.z[t] = *reinterpret_cast<const Pack<uint8_t, SB>*>(z + g0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < SB; ++j) {
+          const int64_t g = std::min(g0 + j, q.ngroups - 1);
+          c.s[t].at[j] = s[g];
+          if (q.zero) c.z[t].at[j] = z[g];
+        }
+      }
+      if (!q.zero)
+#pragma unroll
+        for (int j = 0; j < SB; ++j) c.z[t].at[j] = 8;
     }
+  };
+  auto load_x = [&](uint32x4 (&v)[4], int64_t ch) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int64_t k = ch * 128 + (NG == 1 ? kg * 32 + t * 8 : t * 32 + kg * 8);
-      c.x[t] = uint32x4{0u, 0u, 0u, 0u};
-      if (k < xcols) c.x[t] = load16(xrow + k);
+      v[t] = uint32x4{0u, 0u, 0u, 0u};
+      if (k < q.ncols) v[t] = load16(xrow + k);
     }
   };
   floatx4 sum[RT] = {};
-  Chunk<NG, RT> c;
-  if (wave < chunks) load(c, wave);
-  for (int64_t ch = wave; ch < chunks; ch += waves) {
-    Chunk<NG, RT> next = c;
-    if (ch + waves < chunks) load(next, ch + waves);
-    if constexpr (P == 1)
+  Block c;
+  uint32x4 xn[4];
+  if (b0 < b1) {
+    load(c, b0);
+    load_x(xn, int64_t(b0) * BC);
+  }
+  for (int b = b0; b < b1; ++b) {
+    Block next = c;
+    if (b + 1 < b1) load(next, b + 1);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) c.x[t] = to_code_order(c.x[t]);
-    const uint32x4 ones = {M::kOnes, M::kOnes, M::kOnes, M::kOnes};
-    floatx4 xs[NG] = {};
-    if constexpr (!M::kCentred)
+    for (int ch = 0; ch < BC; ++ch) {
+      uint32x4 xc[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) xs[t * NG / 4] = M::mfma(c.x[t], ones, xs[t * NG / 4]);
+      for (int t = 0; t < 4; ++t) xc[t] = to_code_order(xn[t]);
+      load_x(xn, int64_t(b) * BC + ch + 1);
+      floatx4 xs[NG] = {};
+      if constexpr (!M::kCentred) {
+        const uint32x4 ones = {M::kOnes, M::kOnes, M::kOnes, M::kOnes};
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      uint32x4 w = c.code[t];
-      if constexpr (NG > 1) {
-        const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-        const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-        const auto e = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-        const auto f = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-        w = uint32x4{e[0], e[1], f[0], f[1]};
+        for (int t = 0; t < 4; ++t) xs[t * NG / 4] = M::mfma(xc[t], ones, xs[t * NG / 4]);
       }
 #pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        floatx4 acc = {};
-#pragma unroll
-        for (int k = j * 4 / NG; k < (j + 1) * 4 / NG; ++k) {
-          uint32x4 u = decode<M>(w[k]);
-          if constexpr (M::kCentred) u = centred(u, f16x2{_Float16(c.z[t][j]), _Float16(c.z[t][j])});
-          acc = M::mfma(c.x[k], u, acc);
+      for (int t = 0; t < RT; ++t) {
+        uint32x4 w = c.code[t][ch];
+        if constexpr (NG > 1) {
+          const auto p0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+          const auto p1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+          const auto q0 = __builtin_amdgcn_permlane16_swap(p0[0], p1[0], false, false);
+          const auto q1 = __builtin_amdgcn_permlane16_swap(p0[1], p1[1], false, false);
+          w = uint32x4{q0[0], q0[1], q1[0], q1[1]};
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sum[t][i] = fmaf(c.s[t][j], M::kCentred ? acc[i] : fmaf(-c.z[t][j], xs[j][i], acc[i]),
-                           sum[t][i]);
+        for (int j = 0; j < NG; ++j) {
+          const int g = ch * NG / kSpan + j;
+          const float s = F16::widen(c.s[t].at[g]), z = float(c.z[t].at[g] & 15);
+          floatx4 acc = {};
+#pragma unroll
+          for (int k = j * 4 / NG; k < (j + 1) * 4 / NG; ++k) {
+            uint32x4 u = decode<M>(w[k]);
+            if constexpr (M::kCentred) u = centred(u, f16x2{_Float16(z), _Float16(z)});
+            acc = M::mfma(xc[k], u, acc);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sum[t][i] = fmaf(s, M::kCentred ? acc[i] : fmaf(-z, xs[j][i], acc[i]), sum[t][i]);
+        }
       }
     }
     c = next;
@@ -339,22 +403,16 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx,
   for (int k = int(threadIdx.x); k < nvec * RT * 16; k += int(blockDim.x)) {
     const int rn = k % (16 * RT), v = k / (16 * RT);
     const int64_t r = r0 + rn;
-    float total = 0.f;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int row = P * v + p;
-      const int at = ((rn >> 4) * 4 + (row & 3)) * 64 + (row >> 2) * 16 + (rn & 15);
-      float one = part[at];
-      for (int w = 1; w < waves; ++w) one += part[w * (RT * 256) + at];
-      total += one;
-    }
+    const int at = ((rn >> 4) * 4 + (v & 3)) * 64 + (v >> 2) * 16 + (rn & 15);
+    float total = part[at];
+    for (int w = 1; w < waves; ++w) total += part[w * (RT * 256) + at];
     if (r < q.nrows) store_y(y, ytype, int64_t(v) * ldy + r, total);
   }
 }
 
 // ---------------------------------------------------------------- many vectors
 
-// A workgroup of four waves makes 32 MT vectors x 256 rows, a wave 64 of the rows, in
+// A workgroup of four waves makes 32 MT vectors x 128 RT rows, a wave 32 RT of the rows, in
 // stages of 128 columns on 32x32x16 products. Every wave decodes its own rows' codes in
 // registers (nobody else's), while the vectors' fragments are the same for all four: they
 // are laid out once, by frag_kernel, in the order in which lanes take them, so a stage is
@@ -365,7 +423,6 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx,
 // have changed lanes so that each half of the chunk has two products of its own.
 // Each group's product meets its scale, zero point and sum of x in fp32.
 constexpr int kStage = 128;            // columns
-constexpr int kTileRows = 256;         // of codes, a workgroup
 constexpr int kFragBytes = 1024;       // 64 lanes x 16
 constexpr int kStageFrags = 8;         // a stage of 32 vectors, each piece of x
 constexpr int kTileVecs = 32;
@@ -429,7 +486,7 @@ __device__ __forceinline__ void to_lds4(const void* from, void* to) {
                                    (__attribute__((address_space(3))) void*)(to), 4, 0, 0);
 }
 
-template <class M, int P, int NG, int MT>
+template <class M, int P, int NG, int MT, int RT>
 __global__ void __launch_bounds__(256, P == 1 || MT == 1 ? 2 : 1)
 gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int splits,
             void* __restrict__ y, int ytype, int64_t ldy, float* __restrict__ partial) {
@@ -447,18 +504,18 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
   const int lane = int(threadIdx.x & 63);
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int n = lane & 31, kg = lane >> 5;
-  const int64_t r0 = int64_t(rt) * kTileRows + wave * 64;
-  const uint32_t* crow[2];
-  int64_t grow[2];
+  const int64_t r0 = (int64_t(rt) * 4 + wave) * (32 * RT);
+  const uint32_t* crow[RT];
+  int64_t grow[RT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < RT; ++t) {
     const int64_t r = std::min(r0 + 32 * t + n, q.nrows - 1);
     crow[t] = q.codes + r * q.row_words;
     grow[t] = r * q.ngroups;
   }
   struct Rows {
-    uint32x4 code[2][2];   // rows' tile, chunk
-    float s[2][NG], z[2][NG];
+    uint32x4 code[RT][2];   // rows' tile, chunk
+    float s[RT][NG], z[RT][NG];
   };
   auto fetch = [&](int stage, int buf, Rows& c) __attribute__((always_inline)) {
 #pragma unroll
@@ -475,7 +532,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
                 &sums[buf][wave][0]);
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < RT; ++t) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t w = int64_t(stage) * 16 + h * 8 + kg * 4;
@@ -491,7 +548,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
       }
     }
   };
-  floatx16 total[2][MT] = {};
+  floatx16 total[RT][MT] = {};
   Rows cur;
   fetch(s0, 0, cur);
   for (int s = s0; s < s1; ++s) {
@@ -500,13 +557,15 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
     const int buf = (s - s0) & 1;
     Rows next = cur;
     if (s + 1 < s1) fetch(s + 1, buf ^ 1, next);
-    floatx16 acc[2][MT];
+    floatx16 acc[RT][MT];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32x4 w[2] = {cur.code[0][h], cur.code[1][h]};
+      uint32x4 w[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) w[t] = cur.code[t][h];
       if constexpr (NG == 4) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < RT; ++t) {
           const auto a = __builtin_amdgcn_permlane32_swap(w[t][0], w[t][1], false, false);
           const auto b = __builtin_amdgcn_permlane32_swap(w[t][2], w[t][3], false, false);
           w[t] = uint32x4{a[0], b[0], a[1], b[1]};
@@ -516,9 +575,9 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
       for (int k = 0; k < 4; ++k) {
         constexpr int kEach = 8 / NG;                // products of a group
         const int at = h * 4 + k, j = at / kEach;
-        uint32x4 u[2];
+        uint32x4 u[RT];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < RT; ++t) {
           u[t] = decode<M>(w[t][k]);
           if constexpr (M::kCentred)
             u[t] = centred(u[t], f16x2{_Float16(cur.z[t][j]), _Float16(cur.z[t][j])});
@@ -529,7 +588,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
           for (int p = 0; p < P; ++p) {
             const uint32x4 a = frag[buf][((m * P + p) * kStageFrags + at) * 64 + lane];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < RT; ++t) {
               if (at % kEach == 0 && p == 0) acc[t][m] = M::mfma(a, u[t], floatx16{});
               else acc[t][m] = M::mfma(a, u[t], acc[t][m]);
             }
@@ -543,7 +602,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
               if constexpr (!M::kCentred)
                 xs = *reinterpret_cast<const floatx4*>(&sums[buf][j][m * 32 + 2 * i + 4 * kg]);
 #pragma unroll
-              for (int t = 0; t < 2; ++t)
+              for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const float d = M::kCentred ? acc[t][m][i + e]
@@ -558,7 +617,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
   }
   // register i of lane l: vector 8 (i / 4) + 4 (l / 32) + i % 4, row l % 32
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < RT; ++t) {
     const int64_t r = r0 + 32 * t + n;
     if (r >= q.nrows) continue;
 #pragma unroll
@@ -587,7 +646,7 @@ join_kernel(const float* __restrict__ partial, int splits, int64_t nvec, int64_t
 
 // How a product with many vectors is cut.
 struct GemmPlan {
-  int mt, vec_tiles, row_tiles, splits;
+  int mt, rt, vec_tiles, row_tiles, splits;
   int64_t stages, padded;
   size_t frag_bytes, sum_bytes, total;
 };
@@ -595,11 +654,20 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   GemmPlan p;
   p.mt = nvec <= 32 ? 1 : 2;
   p.vec_tiles = int((nvec + 32 * p.mt - 1) / (32 * p.mt));
-  p.row_tiles = int((nrows + kTileRows - 1) / kTileRows);
+  // 64 rows a wave need as many tiles as the chip holds workgroups: 32000 x 4096 and 512
+  // vectors 172 us (32 rows: 181), in fp32 480 (636); 4096 x 4096 and 64 22.2 (18.6),
+  // 12000 x 1504 and 300 36.9 (29.8).
+  p.rt = (nrows + 255) / 256 * p.vec_tiles >= 512 ? 2 : 1;
+  p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
   p.stages = (ncols + kStage - 1) / kStage;
   p.padded = int64_t(p.vec_tiles) * 32 * p.mt;
   const int64_t tiles = int64_t(p.vec_tiles) * p.row_tiles;
-  p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, p.stages / 4)));
+  // Workgroups for two on each CU, of four stages at least (two in fp32, whose stages take
+  // three times the products); each split more is more to join. 8192 x 28672 and 32
+  // vectors: up to 512 workgroups 52.2 us, 256 74.4, 1024 56.6; 2000 x 8192 and 17: four
+  // stages 16.6, two 19.6; 1001 x 2056 and 100 in fp32: 24.9 and 21.1.
+  p.splits = int(std::max<int64_t>(
+      1, std::min<int64_t>({512 / tiles, p.stages / (pieces == 3 ? 2 : 4), 32})));
   p.frag_bytes = align256(size_t(p.padded / kTileVecs) * p.stages * pieces * kStageFrags * kFragBytes);
   p.sum_bytes = align256(size_t(p.stages) * 4 * p.padded * sizeof(float));
   p.total = p.frag_bytes + p.sum_bytes;
@@ -623,17 +691,20 @@ hipError_t launch_gemm(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, 
     const typename X::raw* x = static_cast<const typename X::raw*>(d_x) + v * ldx;
     void* y = static_cast<char*>(d_y) + v * ldy * (ytype == SEEDQ_F32 ? 4 : 2);
     const unsigned units = unsigned((p.row_tiles * p.splits + 7) / 8 * 8);
-    auto go = [&](auto ng, auto mt) {
-      constexpr int NG = decltype(ng)::value, MT = decltype(mt)::value;
+    auto go = [&](auto ng, auto mt, auto rt) {
+      constexpr int NG = decltype(ng)::value, MT = decltype(mt)::value, RT = decltype(rt)::value;
       hipLaunchKernelGGL((frag_kernel<X, P, !M::kCentred, NG>),
                          dim3(unsigned(p.stages), unsigned(p.padded / kTileVecs)), dim3(256), 0,
                          stream, x, ldx, nv, q.ncols, f);
-      hipLaunchKernelGGL((gemm_kernel<M, P, NG, MT>), dim3(units * unsigned(p.vec_tiles)), dim3(256),
+      hipLaunchKernelGGL((gemm_kernel<M, P, NG, MT, RT>), dim3(units * unsigned(p.vec_tiles)), dim3(256),
                          0, stream, q, nv, f, p.vec_tiles, p.row_tiles, p.splits, y, ytype, ldy,
                          partial);
     };
     auto with_mt = [&](auto ng) {
-      p.mt == 1 ? go(ng, std::integral_constant<int, 1>{}) : go(ng, std::integral_constant<int, 2>{});
+      using One = std::integral_constant<int, 1>;
+      using Two = std::integral_constant<int, 2>;
+      if (p.mt == 1) p.rt == 1 ? go(ng, One{}, One{}) : go(ng, One{}, Two{});
+      else p.rt == 1 ? go(ng, Two{}, One{}) : go(ng, Two{}, Two{});
     };
     if (q.gshift >= 7) with_mt(std::integral_constant<int, 1>{});
     else if (q.gshift == 6) with_mt(std::integral_constant<int, 2>{});
@@ -645,62 +716,90 @@ hipError_t launch_gemm(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, 
   return hipGetLastError();
 }
 
-// The ways: up to 2 vectors, up to 16 rows of x on 16x16x32 products, more.
-bool few(int64_t nvec) { return nvec <= 2; }
-bool batch(int64_t nvec, int xtype) { return nvec * (xtype == SEEDQ_F32 ? 3 : 1) <= 16; }
+// The ways: the vector ALU, 16x16x32 products, the tiles for many vectors. In fp32 the
+// first takes up to four vectors at a time, twice where the codes are few (4096 x 4096
+// and 8 vectors 16.9 us, the tiles 18.9; 32000 x 4096 and 4 36 and 34, and 8 72 and 35).
+enum class Way { kFew, kBatch, kMany };
+Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
+  if (xtype == SEEDQ_F32)
+    return nvec <= 4 || (nvec <= 8 && nrows * ncols <= int64_t(1) << 24) ? Way::kFew : Way::kMany;
+  return nvec <= 2 ? Way::kFew : nvec <= 16 ? Way::kBatch : Way::kMany;
+}
 
 template <class X>
 hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, void* d_y, int ytype,
                       int64_t ldy, hipStream_t stream) {
   using raw = typename X::raw;
-  const int64_t words = (q.ncols + kC - 1) / kC;
-  const unsigned grid = unsigned((q.nrows + kRows - 1) / kRows);
-  const int per = words > 128 ? 4 : words > 64 ? 2 : 1;
-  const int slabs = int((words + 64 * per - 1) / (64 * per));
-  const int waves = std::min(slabs, kMaxWaves);
-  auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), 0, stream, q, static_cast<const raw*>(d_x),
-                       ldx, slabs, d_y, ytype, ldy);
-    return hipGetLastError();
+  const int64_t steps = (q.ncols + kStepCols - 1) / kStepCols;
+  auto go = [&](auto kern, int nv, int rb, int64_t v) {
+    const size_t step_bytes = size_t(nv) * kStepCols * sizeof(raw);
+    const int panel_steps = int(std::min<int64_t>(steps, kPanelBytes / step_bytes));
+    const int64_t batches = (q.nrows + rb - 1) / rb;
+    // Few rows of many columns are shared by several waves (100 x 28672 5.6 us, one wave a
+    // row 9.7).
+    const int slices = int(std::max<int64_t>(
+        1, std::min<int64_t>({1024 / batches, panel_steps >= 4 ? panel_steps : 1, 8})));
+    // Large workgroups where the panel is large, small ones where rows are few: one vector
+    // with 16, 8 and 4 waves takes 36.7, 38.5 and 61.8 us at 8192 x 28672 in fp16, 5.8,
+    // 5.4 and 5.5 at 4096 x 4096 in bf16, 5.3, 4.0 and 3.6 at 1001 x 2056.
+    int waves = batches >= 4096 && panel_steps * step_bytes > (32 << 10) ? 16 : batches >= 2048 ? 8 : 4;
+    waves = std::max(waves, slices) / slices * slices;
+    const int slots = waves / slices;
+    const unsigned grid = unsigned(std::min<int64_t>((batches + slots - 1) / slots, 4096 / waves));
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), panel_steps * step_bytes, stream, q,
+                       static_cast<const raw*>(d_x) + v * ldx, ldx, panel_steps, slices,
+                       static_cast<char*>(d_y) + v * ldy * (ytype == SEEDQ_F32 ? 4 : 2), ytype, ldy);
   };
-  auto words_of = [&](auto nv) {
-    constexpr int NV = decltype(nv)::value;
-    return per == 4   ? go(gemv_few_kernel<X, NV, 4>)
-           : per == 2 ? go(gemv_few_kernel<X, NV, 2>)
-                      : go(gemv_few_kernel<X, NV, 1>);
-  };
-  return nvec == 1 ? words_of(std::integral_constant<int, 1>{})
-                   : words_of(std::integral_constant<int, 2>{});
+  for (int64_t v = 0; v < nvec; v += 4) {
+    const int n = int(std::min<int64_t>(4, nvec - v));
+    // Two rows a wave share what is read of x: 32000 x 4096 21.0 us (one row 24.2), 8192 x
+    // 28672 and one vector 38.3 (36.7), two 42.7 (49.4).
+    const int rb = q.nrows >= 16384 || (n > 1 && q.nrows >= 8192) ? 2 : 1;
+    if (n == 1) rb == 2 ? go(gemv_few_kernel<X, 1, 2>, 1, 2, v) : go(gemv_few_kernel<X, 1, 1>, 1, 1, v);
+    else if (n == 2) rb == 2 ? go(gemv_few_kernel<X, 2, 2>, 2, 2, v) : go(gemv_few_kernel<X, 2, 1>, 2, 1, v);
+    else if constexpr (sizeof(raw) == 4) {
+      if (n == 3) rb == 2 ? go(gemv_few_kernel<X, 3, 2>, 3, 2, v) : go(gemv_few_kernel<X, 3, 1>, 3, 1, v);
+      else rb == 2 ? go(gemv_few_kernel<X, 4, 2>, 4, 2, v) : go(gemv_few_kernel<X, 4, 1>, 4, 1, v);
+    }
+  }
+  return hipGetLastError();
 }
 
-template <class M, int P>
+template <class M>
 hipError_t launch_batch(const Q4& q, int64_t nvec, const uint16_t* x, int64_t ldx, void* d_y, int ytype,
                         int64_t ldy, hipStream_t stream) {
-  const int waves = int(std::min<int64_t>(kMaxWaves, (q.ncols + 127) / 128));
-  auto go = [&](auto ng, auto rt) {
-    constexpr int NG = decltype(ng)::value, RT = decltype(rt)::value;
-    hipLaunchKernelGGL((gemv_batch_kernel<M, P, NG, RT>),
-                       dim3(unsigned((q.nrows + 16 * RT - 1) / (16 * RT))), dim3(64 * waves),
-                       size_t(waves) * RT * 1024, stream, q, int(nvec), x, ldx, d_y, ytype, ldy);
+  // Two tiles of rows a workgroup, which share what is read of x, where that leaves every
+  // CU a workgroup: 8192 x 28672 and 8 vectors 44 us (one tile 58), 4096 x 4096 and 4 7.8
+  // (5.8). With many workgroups four waves: 32000 x 4096 and 8 24.2 (eight 29.8).
+  const bool two = q.nrows >= 32 * 256;
+  auto go = [&](auto bc, auto sb) {
+    constexpr int BC = decltype(bc)::value, SB = decltype(sb)::value;
+    auto launch = [&](auto kern, int rt) {
+      const int64_t groups = (q.nrows + 16 * rt - 1) / (16 * rt), blocks = (q.ncols + 128 * BC - 1) / (128 * BC);
+      const int waves = int(std::min<int64_t>(blocks, groups >= 512 ? 4 : kBatchWaves));
+      hipLaunchKernelGGL(kern, dim3(unsigned(groups)), dim3(64 * waves), size_t(waves) * rt * 1024,
+                         stream, q, int(nvec), x, ldx, d_y, ytype, ldy);
+    };
+    two ? launch(gemv_batch_kernel<M, BC, SB, 2>, 2) : launch(gemv_batch_kernel<M, BC, SB, 1>, 1);
     return hipGetLastError();
   };
-  auto with_rt = [&](auto ng) {
-    return q.nrows >= 32 * 256 ? go(ng, std::integral_constant<int, 2>{})
-                               : go(ng, std::integral_constant<int, 1>{});
-  };
-  return q.gshift >= 7   ? with_rt(std::integral_constant<int, 1>{})
-         : q.gshift == 6 ? with_rt(std::integral_constant<int, 2>{})
-                         : with_rt(std::integral_constant<int, 4>{});
+  using std::integral_constant;
+  const integral_constant<int, 4> four;
+  switch (q.gshift) {
+    case 5: return go(integral_constant<int, 2>{}, integral_constant<int, 8>{});
+    case 6: return go(four, integral_constant<int, 8>{});
+    case 7: return go(four, integral_constant<int, 4>{});
+    case 8: return go(four, integral_constant<int, 2>{});
+    default: return go(four, integral_constant<int, 1>{});
+  }
 }
 
 }  // namespace
 
 // Bytes for up to kMaxRows rows.
 static size_t rows_bytes(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
+  if (way(nrows, ncols, nvec, xtype) != Way::kMany) return 0;
   const int pieces = xtype == SEEDQ_F32 ? 3 : 1;
-  if (few(nvec)) return 0;
-  if (batch(nvec, xtype))
-    return pieces == 1 ? 0 : align256(size_t(nvec) * 3 * q4_row_words(ncols) * kC * sizeof(uint16_t));
   // the last pass may be shorter and cut its columns more often
   size_t need = gemm_plan(nrows, ncols, std::min(nvec, kMaxVecs), pieces).total;
   if (nvec > kMaxVecs && nvec % kMaxVecs)
@@ -717,26 +816,23 @@ size_t q4_gemv_workspace_bytes(int64_t nrows, int64_t ncols, int64_t nvec, int x
 
 static hipError_t launch_rows(const Q4& q, int64_t nvec, const void* d_x, int xtype, int64_t ldx,
                               void* d_y, int ytype, int64_t ldy, void* d_ws, hipStream_t stream) {
-  if (few(nvec))
-    return with_type(xtype, [&](auto t) {
-      return launch_few<decltype(t)>(q, nvec, d_x, ldx, d_y, ytype, ldy, stream);
-    });
-  if (!batch(nvec, xtype))
-    return xtype == SEEDQ_F32
-               ? launch_gemm<F32, Brain, 3>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
-           : xtype == SEEDQ_F16
-               ? launch_gemm<F16, Half, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
-               : launch_gemm<BF16, Brain, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream);
-  if (xtype == SEEDQ_F32) {
-    uint16_t* pieces = static_cast<uint16_t*>(d_ws);
-    hipLaunchKernelGGL(split_kernel, dim3(unsigned((q.row_words + 255) / 256), unsigned(nvec)),
-                       dim3(256), 0, stream, static_cast<const float*>(d_x), ldx, q.ncols,
-                       q.row_words, pieces);
-    return launch_batch<Brain, 3>(q, nvec, pieces, q.row_words * kC, d_y, ytype, ldy, stream);
+  switch (way(q.nrows, q.ncols, nvec, xtype)) {
+    case Way::kFew:
+      return with_type(xtype, [&](auto t) {
+        return launch_few<decltype(t)>(q, nvec, d_x, ldx, d_y, ytype, ldy, stream);
+      });
+    case Way::kBatch: {
+      const uint16_t* x = static_cast<const uint16_t*>(d_x);
+      return xtype == SEEDQ_F16 ? launch_batch<Half>(q, nvec, x, ldx, d_y, ytype, ldy, stream)
+                                : launch_batch<Brain>(q, nvec, x, ldx, d_y, ytype, ldy, stream);
+    }
+    default:
+      return xtype == SEEDQ_F32
+                 ? launch_gemm<F32, Brain, 3>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
+             : xtype == SEEDQ_F16
+                 ? launch_gemm<F16, Half, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
+                 : launch_gemm<BF16, Brain, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream);
   }
-  const uint16_t* x = static_cast<const uint16_t*>(d_x);
-  return xtype == SEEDQ_F16 ? launch_batch<Half, 1>(q, nvec, x, ldx, d_y, ytype, ldy, stream)
-                            : launch_batch<Brain, 1>(q, nvec, x, ldx, d_y, ytype, ldy, stream);
 }
 
 hipError_t launch_q4_gemv(const Q4& q, int64_t nvec, const void* d_x, int xtype, int64_t ldx,
