@@ -29,7 +29,6 @@ constexpr float kCodeScale = 512.f;   // 2^9
 // The 16-bit arithmetic of a kernel. kCentred: codes have their zero point taken off.
 struct Half {
   static constexpr bool kCentred = true;
-  static constexpr uint32_t kOnes = 0x3C003C00u;
   template <bool HIGH>
   __device__ static __forceinline__ f16x2 pair(uint32_t bytes) {
     return __builtin_bit_cast(
@@ -134,7 +133,7 @@ struct FewX {   // 8 columns of x as they lie in LDS
   uint32x4 v[kPlanes];
 };
 
-template <class X, int NV, int RB>
+template <class X, int NV, int RB, bool ZEROS>
 __global__ void __launch_bounds__(64 * kMaxWaves)
 gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int panel_steps, int slices,
                 void* __restrict__ y, int ytype, int64_t ldy) {
@@ -170,16 +169,18 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
       for (int i = 0; i < RB; ++i) {
         c.code[i] = *reinterpret_cast<const uint32x4*>(crow[i] + wl);
         c.s[i] = q.scale[grow[i] + g];
-        c.z[i] = q.zero ? q.zero[grow[i] + g] & 15 : 8;
+        if (ZEROS) c.z[i] = q.zero[grow[i] + g];   // as it lies in memory: nothing waits for it here
       }
     };
     float acc[NV][RB] = {};
     for (int p0 = 0; p0 < steps; p0 += panel_steps) {
       const int p1 = std::min(p0 + panel_steps, steps), n = p1 - p0;
       const int from = p0 + n * slice / slices, to = p0 + n * (slice + 1) / slices;
-      Codes c0, c1;
-      if (some && from < to) fetch(c0, from);
-      if (some && from + 1 < to) fetch(c1, from + 1);
+      Codes c0, c1, c2;
+      if (some && from < to) {
+        fetch(c0, from);
+        fetch(c1, std::min(from + 1, to - 1));
+      }
       if (steps > panel_steps || b0 == int64_t(blockIdx.x) * slots) {
         __syncthreads();   // the panel before is done with
         for (int i = int(threadIdx.x); i < n * 256 * NV; i += int(blockDim.x)) {
@@ -196,13 +197,15 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
         __syncthreads();
       }
       if (!some) continue;
-      for (int step = from; step < to; ++step) {
-        Codes c2 = c1;
-        if (step + 2 < to) fetch(c2, step + 2);
+      auto use = [&](const Codes& c0, int step, Codes& later) __attribute__((always_inline)) {
+        fetch(later, std::min(step + 2, to - 1));   // always, so that the wait for c0 is not for it
         float d[NV][RB] = {};
         f16x2 zz[RB];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) zz[i] = f16x2{_Float16(float(c0.z[i])), _Float16(float(c0.z[i]))};
+        for (int i = 0; i < RB; ++i) {
+          const _Float16 z = ZEROS ? _Float16(float(c0.z[i] & 15)) : _Float16(8.f);
+          zz[i] = f16x2{z, z};
+        }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           float f[NV][8];
@@ -230,8 +233,13 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
         for (int v = 0; v < NV; ++v)
 #pragma unroll
           for (int i = 0; i < RB; ++i) acc[v][i] = fmaf(F16::widen(c0.s[i]), d[v][i], acc[v][i]);
-        c0 = c1;
-        c1 = c2;
+      };
+      for (int step = from; step < to; step += 3) {
+        use(c0, step, c2);
+        if (step + 1 >= to) break;
+        use(c1, step + 1, c0);
+        if (step + 2 >= to) break;
+        use(c2, step + 2, c1);
       }
     }
 #pragma unroll
@@ -422,6 +430,11 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, v
 // 64; product t takes everybody's word t, or, where a group is 32 columns, words that
 // have changed lanes so that each half of the chunk has two products of its own.
 // Each group's product meets its scale, zero point and sum of x in fp32.
+// 32000 x 4096 and 512 bf16 vectors: 172 us, 780 TFLOP/s, where a library product of 16-bit
+// matrices of that kind reaches 1130. Without the loads of codes the rest takes 144, without
+// decoding or the scales 175, without the barriers or the loads to LDS 173; a second
+// stage ahead (three buffers) 190, 16x16x32 products, whose lanes read 64 bytes of a row,
+// 262 (their registers spill).
 constexpr int kStage = 128;            // columns
 constexpr int kFragBytes = 1024;       // 64 lanes x 16
 constexpr int kStageFrags = 8;         // a stage of 32 vectors, each piece of x
@@ -750,17 +763,20 @@ hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, v
                        static_cast<const raw*>(d_x) + v * ldx, ldx, panel_steps, slices,
                        static_cast<char*>(d_y) + v * ldy * (ytype == SEEDQ_F32 ? 4 : 2), ytype, ldy);
   };
-  for (int64_t v = 0; v < nvec; v += 4) {
-    const int n = int(std::min<int64_t>(4, nvec - v));
+  auto rows = [&](auto nv, int64_t v) {
+    constexpr int NV = decltype(nv)::value;
     // Two rows a wave share what is read of x: 32000 x 4096 21.0 us (one row 24.2), 8192 x
     // 28672 and one vector 38.3 (36.7), two 42.7 (49.4).
-    const int rb = q.nrows >= 16384 || (n > 1 && q.nrows >= 8192) ? 2 : 1;
-    if (n == 1) rb == 2 ? go(gemv_few_kernel<X, 1, 2>, 1, 2, v) : go(gemv_few_kernel<X, 1, 1>, 1, 1, v);
-    else if (n == 2) rb == 2 ? go(gemv_few_kernel<X, 2, 2>, 2, 2, v) : go(gemv_few_kernel<X, 2, 1>, 2, 1, v);
-    else if constexpr (sizeof(raw) == 4) {
-      if (n == 3) rb == 2 ? go(gemv_few_kernel<X, 3, 2>, 3, 2, v) : go(gemv_few_kernel<X, 3, 1>, 3, 1, v);
-      else rb == 2 ? go(gemv_few_kernel<X, 4, 2>, 4, 2, v) : go(gemv_few_kernel<X, 4, 1>, 4, 1, v);
-    }
+    const bool two = q.nrows >= 16384 || (NV > 1 && q.nrows >= 8192);
+    if (q.zero) two ? go(gemv_few_kernel<X, NV, 2, true>, NV, 2, v) : go(gemv_few_kernel<X, NV, 1, true>, NV, 1, v);
+    else two ? go(gemv_few_kernel<X, NV, 2, false>, NV, 2, v) : go(gemv_few_kernel<X, NV, 1, false>, NV, 1, v);
+  };
+  for (int64_t v = 0; v < nvec; v += 4) {
+    const int64_t n = nvec - v;
+    if (n == 1) rows(std::integral_constant<int, 1>{}, v);
+    else if (n == 2) rows(std::integral_constant<int, 2>{}, v);
+    else if constexpr (sizeof(raw) == 4)
+      n == 3 ? rows(std::integral_constant<int, 3>{}, v) : rows(std::integral_constant<int, 4>{}, v);
   }
   return hipGetLastError();
 }
