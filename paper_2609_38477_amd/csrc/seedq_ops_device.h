@@ -95,22 +95,28 @@ __device__ __forceinline__ V apart(V v, F f) {   // f on the 32-bit words of v
     return __builtin_bit_cast(V, uint64_t(f(uint32_t(u))) | uint64_t(f(uint32_t(u >> 32))) << 32);
   }
 }
+// One step: from groups of LANES / 2 lanes to groups of LANES.
+template <int LANES, class V, class F>
+__device__ __forceinline__ V lanes_step(V v, F f) {
+  if constexpr (LANES == 2) return f(v, apart(v, [](uint32_t w) { return moved<0xB1>(w); }));
+  if constexpr (LANES == 4) return f(v, apart(v, [](uint32_t w) { return moved<0x4E>(w); }));
+  if constexpr (LANES == 8) return f(v, apart(v, [](uint32_t w) { return moved<0x141>(w); }));
+  if constexpr (LANES == 16) return f(v, apart(v, [](uint32_t w) { return moved<0x140>(w); }));
+  if constexpr (LANES == 32)
+    return f(apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[0]; }),
+             apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[1]; }));
+  if constexpr (LANES == 64)
+    return f(apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[0]; }),
+             apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[1]; }));
+}
 template <int LANES = 64, class V, class F>
 __device__ __forceinline__ V lanes_reduce(V v, F f) {
-  if constexpr (LANES >= 2) v = f(v, apart(v, [](uint32_t w) { return moved<0xB1>(w); }));
-  if constexpr (LANES >= 4) v = f(v, apart(v, [](uint32_t w) { return moved<0x4E>(w); }));
-  if constexpr (LANES >= 8) v = f(v, apart(v, [](uint32_t w) { return moved<0x141>(w); }));
-  if constexpr (LANES >= 16) v = f(v, apart(v, [](uint32_t w) { return moved<0x140>(w); }));
-  if constexpr (LANES >= 32) {
-    const V a = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[0]; });
-    const V b = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[1]; });
-    v = f(a, b);
-  }
-  if constexpr (LANES >= 64) {
-    const V a = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[0]; });
-    const V b = apart(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[1]; });
-    v = f(a, b);
-  }
+  if constexpr (LANES >= 2) v = lanes_step<2>(v, f);
+  if constexpr (LANES >= 4) v = lanes_step<4>(v, f);
+  if constexpr (LANES >= 8) v = lanes_step<8>(v, f);
+  if constexpr (LANES >= 16) v = lanes_step<16>(v, f);
+  if constexpr (LANES >= 32) v = lanes_step<32>(v, f);
+  if constexpr (LANES >= 64) v = lanes_step<64>(v, f);
   return v;
 }
 
