@@ -115,14 +115,17 @@ __device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v)
 
 // ---------------------------------------------------------------- few vectors
 
-// One or two vectors, or up to four in fp32, on the vector ALU. The vectors lie in LDS (a panel of kPanelBytes
-// of them, which is all of them but for very long rows) and the waves go over the rows: RB
+// One or two vectors, or up to four in fp32, on the vector ALU. The vectors lie in LDS (a
+// panel of kPanelBytes, which is all of them but for very long rows) and the waves go over the rows: RB
 // rows a wave at a time, 2048 columns of them a step, 16 bytes of codes a lane, the next
 // steps' codes on their way. A lane's columns lie in one group, so the scale enters once a
 // lane and step. The products u - z (fp16) times x are fused multiply-adds in fp32 that read
 // either half of a register. Where rows are few, `slices` waves share them, each with
 // steps of its own. Order of the sums: the columns of a lane and step, the steps, the
 // lanes as a tree, the slices in order.
+// Memory bounds one vector (8192 x 28672 fp16 27 to 31 us, 4.0 to 4.4 TB/s of codes and
+// scales), the vector ALU more: two take 34 us, four in fp32 58, of which half an
+// operation a product. 4096 x 4096 takes 5.0 us, 1.9 of them an empty launch.
 constexpr int kMaxWaves = 16;
 constexpr int kStepCols = 64 * 4 * kC;
 constexpr int kPanelBytes = 128 << 10;
@@ -753,8 +756,8 @@ hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, v
     const int slices = int(std::max<int64_t>(
         1, std::min<int64_t>({1024 / batches, panel_steps >= 4 ? panel_steps : 1, 8})));
     // Large workgroups where the panel is large, small ones where rows are few: one vector
-    // with 16, 8 and 4 waves takes 36.7, 38.5 and 61.8 us at 8192 x 28672 in fp16, 5.8,
-    // 5.4 and 5.5 at 4096 x 4096 in bf16, 5.3, 4.0 and 3.6 at 1001 x 2056.
+    // with 16, 8 and 4 waves takes 27.6, 28.8 and 41.4 us at 8192 x 28672 in fp16, 5.4,
+    // 5.1 and 5.1 at 4096 x 4096 in bf16, 5.2, 3.9 and 3.5 at 1001 x 2056.
     int waves = batches >= 4096 && panel_steps * step_bytes > (32 << 10) ? 16 : batches >= 2048 ? 8 : 4;
     waves = std::max(waves, slices) / slices * slices;
     const int slots = waves / slices;
@@ -765,8 +768,9 @@ hipError_t launch_few(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, v
   };
   auto rows = [&](auto nv, int64_t v) {
     constexpr int NV = decltype(nv)::value;
-    // Two rows a wave share what is read of x: 32000 x 4096 21.0 us (one row 24.2), 8192 x
-    // 28672 and one vector 38.3 (36.7), two 42.7 (49.4).
+    // Two rows a wave share what is read of x: 32000 x 4096 18.9 us (one row 22.4), 8192 x
+    // 28672 and two vectors 34.5 (36.7), four in fp32 58.3 (70.6); 14336 x 4096 and one
+    // vector 11.6 (11.2), in fp32 10.9 (9.6).
     const bool two = q.nrows >= 16384 || (NV > 1 && q.nrows >= 8192);
     if (q.zero) two ? go(gemv_few_kernel<X, NV, 2, true>, NV, 2, v) : go(gemv_few_kernel<X, NV, 1, true>, NV, 1, v);
     else two ? go(gemv_few_kernel<X, NV, 2, false>, NV, 2, v) : go(gemv_few_kernel<X, NV, 1, false>, NV, 1, v);
