@@ -133,12 +133,14 @@ def _type(dtype, what: str) -> int:
 
 
 def _on(stream):
-    """The stream that a helper allocates and launches on."""
+    """The stream that a helper allocates and launches on; it is one of the current GPU."""
     if stream is None:
         return _current
     import torch
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(stream)
+    if stream.device.index != torch.cuda.current_device():
+        raise ValueError(f"stream: one of GPU {torch.cuda.current_device()} wanted")
     return torch.cuda.stream(stream)
 
 
