@@ -4,10 +4,10 @@
 // consecutive columns, which are one word of codes: a wave covers 512 columns of a
 // row, so every group (32 to 512 columns) lies in 4 to 64 neighbouring lanes of
 // one wave and its extremes are found without LDS. At 8192 x 28672 bf16 in groups of 128 the
-// quantiser takes 133 us (4.4 TB/s) and the decoder 109 us (5.4 TB/s, the rate of a large
+// quantiser takes 129 us (4.6 TB/s) and the decoder 109 us (5.4 TB/s, the rate of a large
 // copy); at 4096 x 14336 fp32 47 us (5.7 TB/s, from the last-level cache in part) and 57 us.
-// What is left over the copy's rate in 16 bits is the arithmetic, some 14 operations a
-// weight, more with zero points: 4096 x 14336 bf16 in groups of 64 takes 44 us with them.
+// What is left over the copy's rate in 16 bits is the arithmetic, some 12 operations a
+// weight, more with zero points: 4096 x 14336 bf16 in groups of 64 takes 41 us with them.
 #include "seedq_ops_device.h"
 
 namespace seedq {
@@ -97,7 +97,11 @@ quantize_kernel(const typename T::raw* __restrict__ W, int64_t ldw, Q4 q, uint32
       float v[8];
       rounded_quotients(w, s, inv, v);   // all 0 where s is
 #pragma unroll
-      for (int i = 0; i < 8; ++i) code |= uint32_t(fminf(fmaxf(v[i] + z, 0.f), 15.f)) << (4 * i);
+      for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i], -z, 15.f - z);
+      // half a word is a whole number below 2^16 in fp32; the zero points join at the end
+      const float low = fmaf(fmaf(fmaf(v[3], 16.f, v[2]), 16.f, v[1]), 16.f, v[0]);
+      const float high = fmaf(fmaf(fmaf(v[7], 16.f, v[6]), 16.f, v[5]), 16.f, v[4]);
+      code = uint32_t(int(low)) + (uint32_t(int(high)) << 16) + uint32_t(z) * 0x11111111u;
     }
     if (word < q.row_words) codes[r * q.row_words + word] = code;   // zero after the last column
     if (c < q.ncols && (lane & (lanes - 1)) == 0) {
