@@ -11,6 +11,7 @@
 // three bf16 pieces of 8 bits (truncated, so that they add up to it exactly) that are
 // multiplied like three vectors: every product is exact and only the fp32 sums round.
 #include <algorithm>
+#include <type_traits>
 
 #include "seedq_ops_device.h"
 
@@ -433,8 +434,9 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, v
 // 64; product t takes everybody's word t, or, where a group is 32 columns, words that
 // have changed lanes so that each half of the chunk has two products of its own.
 // Each group's product meets its scale, zero point and sum of x in fp32.
-// 32000 x 4096 and 512 bf16 vectors: 172 us, 780 TFLOP/s, where a library product of 16-bit
-// matrices of that kind reaches 1130. Without the loads of codes the rest takes 144, without
+// 32000 x 4096 and 512 vectors: 163 us in fp16, 172 to 177 in bf16 (820 and 760 to 780
+// TFLOP/s), where a library product of 16-bit matrices of that kind reaches 1130. In bf16,
+// without the loads of codes the rest takes 144, without
 // decoding or the scales 175, without the barriers or the loads to LDS 173; a second
 // stage ahead (three buffers) 190, 16x16x32 products, whose lanes read 64 bytes of a row,
 // 262 (their registers spill).
@@ -507,6 +509,10 @@ __global__ void __launch_bounds__(256, P == 1 || MT == 1 ? 2 : 1)
 gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int splits,
             void* __restrict__ y, int ytype, int64_t ldy, float* __restrict__ partial) {
   constexpr int kFrags = MT * P * kStageFrags;
+  // Scales and zero points kept as they lie in memory do not wait for their load at once
+  // (32000 x 4096 and 512 vectors in groups of 64 256 -> 239 us); in groups of 32 their
+  // conversions cost more than that (273 -> 302).
+  constexpr bool kRaw = NG < 4;
   __shared__ __attribute__((aligned(16))) uint32x4 frag[2][kFrags * 64];
   __shared__ __attribute__((aligned(16))) float sums[2][NG][MT * kTileVecs];
   // Workgroups go to the eight XCDs in turn: those of one XCD that run together share
@@ -531,7 +537,16 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
   }
   struct Rows {
     uint32x4 code[RT][2];   // rows' tile, chunk
-    float s[RT][NG], z[RT][NG];
+    std::conditional_t<kRaw, uint16_t, float> s[RT][NG];
+    std::conditional_t<kRaw, uint8_t, float> z[RT][NG];
+  };
+  auto scale_of = [](auto s) {
+    if constexpr (kRaw) return F16::widen(s);
+    else return s;
+  };
+  auto zero_of = [](auto z) {
+    if constexpr (kRaw) return float(z & 15);
+    else return z;
   };
   auto fetch = [&](int stage, int buf, Rows& c) __attribute__((always_inline)) {
 #pragma unroll
@@ -552,15 +567,20 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t w = int64_t(stage) * 16 + h * 8 + kg * 4;
-        c.code[t][h] = uint32x4{0u, 0u, 0u, 0u};
-        if (w < q.row_words) c.code[t][h] = *reinterpret_cast<const uint32x4*>(crow[t] + w);
+        // past the last column the row's start: x is zero there
+        c.code[t][h] = *reinterpret_cast<const uint32x4*>(crow[t] + (w < q.row_words ? w : 0));
       }
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         const int64_t g = grow[t] + std::min((int64_t(stage) * kStage + j * (kStage / NG)) >> q.gshift,
                                              q.ngroups - 1);
-        c.s[t][j] = F16::widen(q.scale[g]);
-        c.z[t][j] = q.zero ? float(q.zero[g] & 15) : 8.f;
+        if constexpr (kRaw) {
+          c.s[t][j] = q.scale[g];
+          c.z[t][j] = q.zero ? q.zero[g] : uint8_t(8);
+        } else {
+          c.s[t][j] = F16::widen(q.scale[g]);
+          c.z[t][j] = q.zero ? float(q.zero[g] & 15) : 8.f;
+        }
       }
     }
   };
@@ -596,7 +616,10 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
         for (int t = 0; t < RT; ++t) {
           u[t] = decode<M>(w[t][k]);
           if constexpr (M::kCentred)
-            u[t] = centred(u[t], f16x2{_Float16(cur.z[t][j]), _Float16(cur.z[t][j])});
+            {
+            const _Float16 z = _Float16(zero_of(cur.z[t][j]));
+            u[t] = centred(u[t], f16x2{z, z});
+          }
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -622,8 +645,8 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const float d = M::kCentred ? acc[t][m][i + e]
-                                              : fmaf(-cur.z[t][j], xs[e], acc[t][m][i + e]);
-                  total[t][m][i + e] = fmaf(cur.s[t][j], d, total[t][m][i + e]);
+                                              : fmaf(-zero_of(cur.z[t][j]), xs[e], acc[t][m][i + e]);
+                  total[t][m][i + e] = fmaf(scale_of(cur.s[t][j]), d, total[t][m][i + e]);
                 }
             }
         }
@@ -671,7 +694,7 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   p.mt = nvec <= 32 ? 1 : 2;
   p.vec_tiles = int((nvec + 32 * p.mt - 1) / (32 * p.mt));
   // 64 rows a wave need as many tiles as the chip holds workgroups: 32000 x 4096 and 512
-  // vectors 172 us (32 rows: 181), in fp32 480 (636); 4096 x 4096 and 64 22.2 (18.6),
+  // vectors 172 us (32 rows: 181), in fp32 470 (636); 4096 x 4096 and 64 22.2 (18.2),
   // 12000 x 1504 and 300 36.9 (29.8).
   p.rt = (nrows + 255) / 256 * p.vec_tiles >= 512 ? 2 : 1;
   p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
