@@ -279,8 +279,8 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
   T at[N];
 };
 
-// Up to 16 vectors of 16 bits on the matrix core, D = X W^T: a 16x16x32 product takes 16 rows of x and 16 rows of codes. A lane
-// reads 16 bytes of codes of row l % 16, columns 32 (l / 16) .. of a chunk of 128. Where
+// Up to 16 vectors of 16 bits on the matrix core, D = X W^T: a 16x16x32 product takes 16
+// rows of x and 16 rows of codes. A lane reads 16 bytes of codes of row l % 16, columns 32 (l / 16) .. of a chunk of 128. Where
 // a group is 128 columns or more, product t takes everybody's word t; in smaller groups
 // the words first change lanes so that product t holds columns 32 t .. 32 t + 31 (four
 // lane swaps). Each group's product and, in bf16, sum of x (a product with ones) meet in
@@ -288,6 +288,10 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
 // its columns in blocks of BC chunks and add their sums through LDS in order. A block has
 // SB scales a row, which a lane reads at once; its codes are read while the block before
 // is multiplied, x a chunk ahead.
+// 8192 x 28672 and 8 fp16 vectors take 42 to 45 us (2.9 TB/s of codes). Loads are answered in
+// order, so those of x wait behind the next block's codes: without them it takes 36, without
+// decoding as well 26, which is the memory's. The vectors laid out in LDS instead, for a
+// split of the columns each, and the splits joined: 43 to 48 us, at 4096 x 4096 twice as long.
 constexpr int kBatchWaves = 8;
 
 template <class M, int BC, int SB, int RT>
