@@ -435,14 +435,23 @@ int segments(int64_t nrows, int64_t vocab, int per_vector) {
 
 }  // namespace
 
-size_t token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int top) {
+// Bytes for up to kMaxRows rows.
+static size_t rows_bytes(int64_t nrows, int64_t vocab, int top) {
   const int segs = segments(nrows, vocab, 4);   // the type with the most
   if (segs == 1) return 0;
   return partial_bytes(nrows, segs) + align256(size_t(nrows) * segs * top * sizeof(Key));
 }
 
+size_t token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int top) {
+  size_t need = rows_bytes(std::min(nrows, kMaxRows), vocab, top);
+  // the last launch of many may have few rows and cut them
+  if (nrows > kMaxRows && nrows % kMaxRows)
+    need = std::max(need, rows_bytes(nrows % kMaxRows, vocab, top));
+  return need;
+}
+
 hipError_t launch_token_logprobs(const LogprobArgs& all, int type, void* d_ws, hipStream_t stream) {
-  if (all.nrows > kMaxRows) {   // never in segments
+  if (all.nrows > kMaxRows) {   // the launches follow each other and share the workspace
     for (int64_t r = 0; r < all.nrows; r += kMaxRows) {
       const auto from = [&](auto* p, int64_t each) { return p ? p + r * each : p; };
       LogprobArgs a = all;

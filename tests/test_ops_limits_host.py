@@ -1,0 +1,25 @@
+"""Limits of the operators of seedq_ops.h that a GPU's memory does not reach, by what the
+library says of them without a GPU."""
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def sq():
+    import paper_2609_38477_amd as sq
+    if not os.path.exists(sq.LIB_PATH):
+        from paper_2609_38477_amd import build
+        build.build()
+    return sq
+
+
+@pytest.mark.parametrize("vocab,top", [(131072, 5), (65536, 0), (1 << 20, 32), (32000, 20)])
+@pytest.mark.parametrize("left", [1, 37, 128, 200])
+def test_logprobs_workspace_covers_the_last_launch(sq, vocab, top, left):
+    # rows go to launches of 2^21; the last one has `left` rows and may cut them in segments
+    # as a call of so few rows does
+    alone = sq.seedq_token_logprobs_workspace_bytes(left, vocab, top)
+    for launches in (1, 3):
+        assert sq.seedq_token_logprobs_workspace_bytes((launches << 21) + left, vocab, top) == alone
+        assert sq.seedq_token_logprobs_workspace_bytes(launches << 21, vocab, top) == 0
