@@ -457,44 +457,47 @@ struct Frags {
   int64_t stages, padded;   // padded: vectors, a multiple of 64
 };
 
-// A workgroup: 32 vectors, one stage.
+// A workgroup: 32 vectors, a stage at a time.
 template <class X, int P, bool SUMS, int NG>
 __global__ void __launch_bounds__(256)
 frag_kernel(const typename X::raw* __restrict__ x, int64_t ldx, int64_t nvec, int64_t ncols, Frags f) {
   __shared__ float part[kTileVecs][17];
-  const int64_t stage = blockIdx.x, tile = blockIdx.y;
+  const int64_t tile = blockIdx.y;
+  for (int64_t stage = blockIdx.x; stage < f.stages; stage += gridDim.x) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int item = int(threadIdx.x) + 256 * h;   // 16 neighbours: the 128 columns of a vector
-    const int m = item >> 4, w = item & 15;
-    const int64_t v = tile * kTileVecs + m, c = stage * kStage + w * kC;
-    const bool some = v < nvec && c < ncols;
-    uint32x4 piece[3] = {};
-    float sum = 0.f;
-    if (some) {
-      if constexpr (P == 3 || SUMS) {
-        float e[8];
-        load8<X>(x + v * ldx + c, e);
-        sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-        if constexpr (P == 3) split8(e, piece);
+    for (int h = 0; h < 2; ++h) {
+      const int item = int(threadIdx.x) + 256 * h;   // 16 neighbours: the 128 columns of a vector
+      const int m = item >> 4, w = item & 15;
+      const int64_t v = tile * kTileVecs + m, c = stage * kStage + w * kC;
+      const bool some = v < nvec && c < ncols;
+      uint32x4 piece[3] = {};
+      float sum = 0.f;
+      if (some) {
+        if constexpr (P == 3 || SUMS) {
+          float e[8];
+          load8<X>(x + v * ldx + c, e);
+          sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+          if constexpr (P == 3) split8(e, piece);
+        }
+        if constexpr (P == 1) piece[0] = to_code_order(load16(x + v * ldx + c));
       }
-      if constexpr (P == 1) piece[0] = to_code_order(load16(x + v * ldx + c));
+      const int chunk = w >> 3, k = w & 7;
+      const int t = NG == 4 ? k >> 1 : k & 3, lane = (NG == 4 ? k & 1 : k >> 2) * 32 + m;
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        f.frag[(((tile * f.stages + stage) * P + p) * kStageFrags + chunk * 4 + t) * 64 + lane] = piece[p];
+      if (SUMS) part[m][w] = sum;
     }
-    const int chunk = w >> 3, k = w & 7;
-    const int t = NG == 4 ? k >> 1 : k & 3, lane = (NG == 4 ? k & 1 : k >> 2) * 32 + m;
+    if (!SUMS) continue;
+    __syncthreads();
+    if (threadIdx.x < kTileVecs * NG) {
+      const int m = int(threadIdx.x) % kTileVecs, j = int(threadIdx.x) / kTileVecs;
+      float sum = 0.f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      f.frag[(((tile * f.stages + stage) * P + p) * kStageFrags + chunk * 4 + t) * 64 + lane] = piece[p];
-    if (SUMS) part[m][w] = sum;
-  }
-  if (!SUMS) return;
-  __syncthreads();
-  if (threadIdx.x < kTileVecs * NG) {
-    const int m = int(threadIdx.x) % kTileVecs, j = int(threadIdx.x) / kTileVecs;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16 / NG; ++i) sum += part[m][j * (16 / NG) + i];
-    f.sums[(stage * NG + j) * f.padded + tile * kTileVecs + m] = sum;
+      for (int i = 0; i < 16 / NG; ++i) sum += part[m][j * (16 / NG) + i];
+      f.sums[(stage * NG + j) * f.padded + tile * kTileVecs + m] = sum;
+    }
+    __syncthreads();   // the next stage's sums go to the same place
   }
 }
 
@@ -720,6 +723,9 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
 
 // Vectors of one pass: the grids of the kernels below stay small, and so does the workspace.
 constexpr int64_t kMaxVecs = 32768;
+// Stages in one go of frag_kernel: a grid has fewer than 2^32 threads along a dimension, and
+// a stage takes 256.
+constexpr int64_t kMaxStages = int64_t(1) << 20;
 
 template <class X, class M, int P>
 hipError_t launch_gemm(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, void* d_y, int ytype,
@@ -737,7 +743,8 @@ hipError_t launch_gemm(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, 
     auto go = [&](auto ng, auto mt, auto rt) {
       constexpr int NG = decltype(ng)::value, MT = decltype(mt)::value, RT = decltype(rt)::value;
       hipLaunchKernelGGL((frag_kernel<X, P, !M::kCentred, NG>),
-                         dim3(unsigned(p.stages), unsigned(p.padded / kTileVecs)), dim3(256), 0,
+                         dim3(unsigned(std::min(p.stages, kMaxStages)), unsigned(p.padded / kTileVecs)),
+                         dim3(256), 0,
                          stream, x, ldx, nv, q.ncols, f);
       hipLaunchKernelGGL((gemm_kernel<M, P, NG, MT, RT>), dim3(units * unsigned(p.vec_tiles)), dim3(256),
                          0, stream, q, nv, f, p.vec_tiles, p.row_tiles, p.splits, y, ytype, ldy,
