@@ -82,6 +82,7 @@ int seedq_q4_dequantize(const uint32_t* d_codes, const void* d_scale, const uint
  *        or xtype. Not overlapping d_x.
  *   d_workspace: seedq_q4_gemv_workspace_bytes(...) bytes, 256-byte aligned (may be
  *        NULL when that is 0).
+ * They pass the range of fp32 only where sums of s (u - z) x do.
  * A vector with a NaN or an infinity gives outputs that are not finite.
  * Asynchronous on hip_stream. Errors: SEEDQ_EINVAL, SEEDQ_EUNSUPPORTED (group or
  * type), SEEDQ_EWORKSPACE, SEEDQ_EHIP.

@@ -4,7 +4,10 @@
 //     sum over groups g of s_g sum (u - z_g) x = s_g (sum u x - z_g sum x).
 // A byte 0 .. 15 read as an 8-bit float with three mantissa bits stands for u 2^-9 (its
 // subnormals and its first binade), so three operations spread the codes of a word over
-// bytes and four conversions, which also scale, make eight exact 16-bit floats. Their
+// bytes and four conversions, which also scale, make eight exact 16-bit floats. They are
+// made u 2^-11: a sum over the at most 128 columns that meet before the scale stays within
+// 15 / 16 of the largest |x| and cannot overflow where the weights' own products would not;
+// what is stored takes the factor back. Their
 // pairs are columns (0, 2), (4, 6), (1, 3), (5, 7); x is put in that order. In fp16 one
 // packed addition takes z off exactly. In bf16, which has none, the kernels form sum u x
 // and take z sum x from it in fp32 once a group. x in fp32 goes to the matrix core as
@@ -25,7 +28,13 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr float kCodeScale = 512.f;   // 2^9
+constexpr float kUnit = 0x1p-11f;             // a code 1 in the products
+constexpr float kCodeScale = 512.f * kUnit;
+// A zero point as the codes stand in fp16.
+__device__ __forceinline__ f16x2 half_zero(float z) {
+  const _Float16 h = _Float16(z * kUnit);
+  return f16x2{h, h};
+}
 
 // The 16-bit arithmetic of a kernel. kCentred: codes have their zero point taken off.
 struct Half {
@@ -46,7 +55,7 @@ struct Half {
 };
 struct Brain {
   static constexpr bool kCentred = false;
-  static constexpr uint32_t kOnes = 0x3F803F80u;
+  static constexpr uint32_t kOnes = 0x3A003A00u;   // two of kUnit
   template <bool HIGH>
   __device__ static __forceinline__ bf16x2 pair(uint32_t bytes) {
     return __builtin_bit_cast(
@@ -109,7 +118,9 @@ __device__ __forceinline__ void split8(const float (&f)[8], uint32x4 (&piece)[3]
       piece[p][j] = __builtin_amdgcn_perm(h[p][kOrder[2 * j + 1]], h[p][kOrder[2 * j]], 0x07060302u);
 }
 
+// v: a row's sum, in units of kUnit.
 __device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v) {
+  v *= 1.f / kUnit;
   if (ytype == SEEDQ_F32) static_cast<float*>(y)[at] = v;
   else static_cast<uint16_t*>(y)[at] = ytype == SEEDQ_F16 ? F16::narrow(v) : BF16::narrow(v);
 }
@@ -206,10 +217,7 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
         float d[NV][RB] = {};
         f16x2 zz[RB];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) {
-          const _Float16 z = ZEROS ? _Float16(float(c0.z[i] & 15)) : _Float16(8.f);
-          zz[i] = f16x2{z, z};
-        }
+        for (int i = 0; i < RB; ++i) zz[i] = half_zero(ZEROS ? float(c0.z[i] & 15) : 8.f);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           float f[NV][8];
@@ -399,7 +407,7 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, v
 #pragma unroll
           for (int k = j * 4 / NG; k < (j + 1) * 4 / NG; ++k) {
             uint32x4 u = decode<M>(w[k]);
-            if constexpr (M::kCentred) u = centred(u, f16x2{_Float16(z), _Float16(z)});
+            if constexpr (M::kCentred) u = centred(u, half_zero(z));
             acc = M::mfma(xc[k], u, acc);
           }
 #pragma unroll
@@ -450,7 +458,7 @@ constexpr int kStageFrags = 8;         // a stage of 32 vectors, each piece of x
 constexpr int kTileVecs = 32;
 
 // What the vectors are made into: fragments [vector tile][stage][piece][8][lane] of 16
-// bytes and, for codes that keep their zero point, sums of x [stage][NG][padded vectors].
+// bytes and, for codes that keep their zero point, sums of kUnit x [stage][NG][padded vectors].
 struct Frags {
   uint32x4* frag;
   float* sums;
@@ -476,8 +484,10 @@ frag_kernel(const typename X::raw* __restrict__ x, int64_t ldx, int64_t nvec, in
         if constexpr (P == 3 || SUMS) {
           float e[8];
           load8<X>(x + v * ldx + c, e);
-          sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
           if constexpr (P == 3) split8(e, piece);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) e[i] *= kUnit;
+          sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         }
         if constexpr (P == 1) piece[0] = to_code_order(load16(x + v * ldx + c));
       }
@@ -622,11 +632,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           u[t] = decode<M>(w[t][k]);
-          if constexpr (M::kCentred)
-            {
-            const _Float16 z = _Float16(zero_of(cur.z[t][j]));
-            u[t] = centred(u[t], f16x2{z, z});
-          }
+          if constexpr (M::kCentred) u[t] = centred(u[t], half_zero(zero_of(cur.z[t][j])));
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
