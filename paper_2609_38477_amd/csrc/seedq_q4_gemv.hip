@@ -10,9 +10,13 @@
 // what is stored takes the factor back. Their
 // pairs are columns (0, 2), (4, 6), (1, 3), (5, 7); x is put in that order. In fp16 one
 // packed addition takes z off exactly. In bf16, which has none, the kernels form sum u x
-// and take z sum x from it in fp32 once a group. x in fp32 goes to the matrix core as
-// three bf16 pieces of 8 bits (truncated, so that they add up to it exactly) that are
-// multiplied like three vectors: every product is exact and only the fp32 sums round.
+// and take z sum x from it in fp32 once a group; vectors of one sign, whose sums of u x are
+// many times the result, cost that form a few units of fp32 (4096 x 4096 and 64 vectors:
+// 5e-7 of the result's norm, of both signs 8e-8; sums of the decoded weights' products in
+// fp32 4e-7). x in fp32 goes to the matrix core as three bf16 pieces of 8 bits (truncated,
+// so that they add up to it exactly) that are multiplied like three vectors, by codes whose
+// zero point is taken off byte by byte before the conversion: every product is exact and
+// only the fp32 sums round.
 #include <algorithm>
 #include <type_traits>
 
@@ -71,20 +75,42 @@ struct Brain {
   }
 };
 
-// The eight codes of a word as 16-bit floats in code order.
+// bf16 with the zero point off the bytes: 12 operations a word more.
+struct Exact : Brain {
+  static constexpr bool kCentred = true;
+};
+
+// Four bytes as 16-bit floats each, from even and odd codes: a word in code order.
 template <class M>
-__device__ __forceinline__ uint32x4 decode(uint32_t w) {
-  const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+__device__ __forceinline__ uint32x4 to_floats(uint32_t even, uint32_t odd) {
   return uint32x4{__builtin_bit_cast(uint32_t, M::template pair<false>(even)),
                   __builtin_bit_cast(uint32_t, M::template pair<true>(even)),
                   __builtin_bit_cast(uint32_t, M::template pair<false>(odd)),
                   __builtin_bit_cast(uint32_t, M::template pair<true>(odd))};
 }
-__device__ __forceinline__ uint32x4 centred(uint32x4 u, f16x2 z) {
+// u - z of four bytes, each as sign and magnitude (an 8-bit float's bits). z: four times.
+__device__ __forceinline__ uint32_t differences(uint32_t u, uint32_t z) {
+  const uint32_t d = ((u | 0x80808080u) - z) ^ 0x80808080u;   // bytes in two's complement
+  const uint32_t minus = d & 0x80808080u, one = minus >> 7;
+  return (d ^ (minus - one)) + one;
+}
+// The eight codes of a word as 16-bit floats in code order, without their zero point where
+// M is centred.
+template <class M>
+__device__ __forceinline__ uint32x4 decode(uint32_t w, float z) {
+  const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+  if constexpr (std::is_same_v<M, Exact>) {
+    const uint32_t zs = uint32_t(z) * 0x01010101u;
+    return to_floats<M>(differences(even, zs), differences(odd, zs));
+  }
+  uint32x4 u = to_floats<M>(even, odd);
+  if constexpr (std::is_same_v<M, Half>) {
+    const f16x2 zz = half_zero(z);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t pair = u[j];   // a bit cast of a vector's element takes element 0
-    u[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - z);
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t pair = u[j];   // a bit cast of a vector's element takes element 0
+      u[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - zz);
+    }
   }
   return u;
 }
@@ -215,9 +241,9 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
       auto use = [&](const Codes& c0, int step, Codes& later) __attribute__((always_inline)) {
         fetch(later, std::min(step + 2, to - 1));   // always, so that the wait for c0 is not for it
         float d[NV][RB] = {};
-        f16x2 zz[RB];
+        float z[RB];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) zz[i] = half_zero(ZEROS ? float(c0.z[i] & 15) : 8.f);
+        for (int i = 0; i < RB; ++i) z[i] = ZEROS ? float(c0.z[i] & 15) : 8.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           float f[NV][8];
@@ -228,7 +254,7 @@ gemv_few_kernel(Q4 q, const typename X::raw* __restrict__ x, int64_t ldx, int pa
               widen<X>(panel[(((step - p0) * kPlanes + k) * NV + v) * 256 + w * 64 + lane], f[v] + 4 * k);
 #pragma unroll
           for (int i = 0; i < RB; ++i) {
-            const uint32x4 u = centred(decode<Half>(c0.code[i][w]), zz[i]);
+            const uint32x4 u = decode<Half>(c0.code[i][w], z[i]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const uint32_t bits = u[j];
@@ -406,9 +432,7 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, v
           floatx4 acc = {};
 #pragma unroll
           for (int k = j * 4 / NG; k < (j + 1) * 4 / NG; ++k) {
-            uint32x4 u = decode<M>(w[k]);
-            if constexpr (M::kCentred) u = centred(u, half_zero(z));
-            acc = M::mfma(xc[k], u, acc);
+            acc = M::mfma(xc[k], decode<M>(w[k], z), acc);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -610,7 +634,9 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
     const int buf = (s - s0) & 1;
     Rows next = cur;
     if (s + 1 < s1) fetch(s + 1, buf ^ 1, next);
-    floatx16 acc[RT][MT];
+    // The pieces after the first have sums of their own: added to its sums, which are 2^8
+    // times theirs, each would cost a rounding of the whole.
+    floatx16 acc[RT][MT], low[P == 1 ? 1 : RT][P == 1 ? 1 : MT];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint32x4 w[RT];
@@ -630,10 +656,7 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
         const int at = h * 4 + k, j = at / kEach;
         uint32x4 u[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          u[t] = decode<M>(w[t][k]);
-          if constexpr (M::kCentred) u[t] = centred(u[t], half_zero(zero_of(cur.z[t][j])));
-        }
+        for (int t = 0; t < RT; ++t) u[t] = decode<M>(w[t][k], zero_of(cur.z[t][j]));
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -641,8 +664,8 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
             const uint32x4 a = frag[buf][((m * P + p) * kStageFrags + at) * 64 + lane];
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-              if (at % kEach == 0 && p == 0) acc[t][m] = M::mfma(a, u[t], floatx16{});
-              else acc[t][m] = M::mfma(a, u[t], acc[t][m]);
+              floatx16& to = p == 0 ? acc[t][m] : low[t][m];
+              to = M::mfma(a, u[t], at % kEach == 0 && p < 2 ? floatx16{} : to);
             }
           }
         if (at % kEach == kEach - 1) {
@@ -657,8 +680,9 @@ gemm_kernel(Q4 q, int64_t nvec, Frags f, int vec_tiles, int row_tiles, int split
               for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                  const float d = M::kCentred ? acc[t][m][i + e]
-                                              : fmaf(-zero_of(cur.z[t][j]), xs[e], acc[t][m][i + e]);
+                  float d = acc[t][m][i + e];
+                  if constexpr (P > 1) d += low[t][m][i + e];
+                  if constexpr (!M::kCentred) d = fmaf(-zero_of(cur.z[t][j]), xs[e], d);
                   total[t][m][i + e] = fmaf(scale_of(cur.s[t][j]), d, total[t][m][i + e]);
                 }
             }
@@ -721,7 +745,7 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   p.splits = int(std::max<int64_t>(
       1, std::min<int64_t>({512 / tiles, p.stages / (pieces == 3 ? 2 : 4), 32})));
   p.frag_bytes = align256(size_t(p.padded / kTileVecs) * p.stages * pieces * kStageFrags * kFragBytes);
-  p.sum_bytes = align256(size_t(p.stages) * 4 * p.padded * sizeof(float));
+  p.sum_bytes = pieces == 3 ? 0 : align256(size_t(p.stages) * 4 * p.padded * sizeof(float));
   p.total = p.frag_bytes + p.sum_bytes;
   if (p.splits > 1) p.total += align256(size_t(p.splits) * nvec * nrows * sizeof(float));
   return p;
@@ -888,7 +912,7 @@ static hipError_t launch_rows(const Q4& q, int64_t nvec, const void* d_x, int xt
     }
     default:
       return xtype == SEEDQ_F32
-                 ? launch_gemm<F32, Brain, 3>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
+                 ? launch_gemm<F32, Exact, 3>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
              : xtype == SEEDQ_F16
                  ? launch_gemm<F16, Half, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream)
                  : launch_gemm<BF16, Brain, 1>(q, nvec, d_x, ldx, d_y, ytype, ldy, d_ws, stream);
