@@ -128,8 +128,10 @@ int seedq_token_logprobs(const void* d_logits, int32_t type, int64_t ld, int64_t
  * Gradient of sum_t (g_t logprob_t + h_t entropy_t) at the logits, from the lse and
  * entropy that seedq_token_logprobs gave:
  *   dx_v = g (1[v = token] - p_v) - h p_v (log p_v + entropy),  p_v = e^(x_v - lse),
- * rounded once to the logits' type. p is 0 at -inf (the gradient there is g at the
- * token itself, else 0). A row without any finite logit (lse -inf) has gradient 0;
+ * rounded once to the logits' type. Where |lse| >= 1024, which fp32 holds too coarsely
+ * for p (a row of nothing but the type's lowest value: log S is lost), p is taken from
+ * the row's own m and S, at the price of a second pass over it. p is 0 at -inf (the
+ * gradient there is g at the token itself, else 0). A row without any finite logit (lse -inf) has gradient 0;
  * a NaN lse gives NaN. A negative token has no log probability to differentiate; one
  * >= vocab gives a NaN row.
  *   d_grad_logprob (g), d_grad_entropy (h): fp32 [nrows], at least one not NULL;

@@ -361,11 +361,52 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(LogprobArgs a, int s
 // ---------------------------------------------------------------- gradient
 
 constexpr int kGradThreads = 256;
+// An lse in fp32 errs by 2^-24 of itself, and e^(x - lse) by as much of 1: from here on by
+// 2^-14 and more, all of it in a row of the type's lowest value. Such a row's p are taken
+// from its own largest logit and sum.
+constexpr float kFarLse = 1024.f;
+
+// The largest logit of a row and the log of its sum relative to it, for all threads, by one
+// workgroup that has read the whole row when this returns.
+template <class T>
+__device__ __forceinline__ void largest_and_log_sum(const Row<T>& row, float& m, float& log_s) {
+  constexpr int kWaves = kGradThreads / 64;
+  __shared__ float sm[kWaves];
+  __shared__ double ss[kWaves];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Sums s;
+#pragma unroll 1
+  for (uint32_t i = tid; i < row.vectors; i += kGradThreads) {
+    float f[kPerVector<T>];
+    widen<T>(row.load(i), f);
+    s.raise(largest(f));
+#pragma unroll
+    for (int k = 0; k < kPerVector<T>; ++k) s.add(f[k]);
+  }
+  if (tid < row.tail) {
+    const float x = T::widen(row.x[row.vectors * kPerVector<T> + tid]);
+    s.raise(x);
+    s.add(x);
+  }
+  m = lanes_reduce(s.m, [](float p, float q) { return fmaxf(p, q); });
+  if (lane == 0) sm[wave] = m;
+  __syncthreads();
+  m = sm[0];
+  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w]);
+  const double c = __builtin_amdgcn_exp2f(fmaxf(s.m - m, kFar) * kLog2E);
+  double S = lanes_reduce(c * s.S, [](double p, double q) { return p + q; });
+  if (lane == 0) ss[wave] = S;
+  __syncthreads();
+  S = ss[0];
+  for (int w = 1; w < kWaves; ++w) S += ss[w];
+  log_s = float(log(S));
+}
 
 struct GradRow {
   float lse, g, h, H;
+  float m = 0.f, log_s = 0.f;   // lse in two parts, in a far row
   int64_t tok;
-  bool empty, outside;
+  bool empty, outside, far;
   __device__ GradRow(const LogprobGradArgs& a, int64_t t) {
     lse = a.lse[t];
     tok = a.tokens ? a.tokens[t] : -1;
@@ -374,9 +415,11 @@ struct GradRow {
     h = a.h ? a.h[t] : 0.f;
     H = a.h ? a.entropy[t] : 0.f;
     empty = lse == -kInf;
+    far = fabsf(lse) >= kFarLse && fabsf(lse) < kInf;
   }
+  template <bool FAR>
   __device__ __forceinline__ float at(float x, int64_t v) const {
-    const float lp = x - lse;
+    const float lp = FAR ? (x - m) - log_s : x - lse;
     const float p = __builtin_amdgcn_exp2f(lp * kLog2E);
     float d = v == tok ? g : 0.f;
     if (p != 0.f) d -= p * fmaf(h, lp + H, g);   // a NaN counts as different from 0
@@ -384,21 +427,18 @@ struct GradRow {
   }
 };
 
-// A workgroup takes kUnroll vectors a thread of one row at a time.
-template <class T>
-__global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(LogprobGradArgs a) {
+// The gradients of a row's vectors from `first` on, kUnroll a thread and step of `by`
+// vectors, and of the elements after the last vector.
+template <class T, bool FAR>
+__device__ __forceinline__ void write_gradient(const Row<T>& row, const GradRow& r,
+                                               typename T::raw* out, int64_t first, int64_t by) {
   constexpr int N = kPerVector<T>;
-  const int64_t t = blockIdx.x;
-  const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
-  typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
-  const GradRow r(a, t);
   const uint32_t tid = threadIdx.x;
-  if (blockIdx.y == 0 && tid < row.tail) {
+  if (first == 0 && tid < row.tail) {
     const uint32_t e = row.vectors * N + tid;
-    out[e] = T::narrow(r.at(T::widen(row.x[e]), e));
+    out[e] = T::narrow(r.template at<FAR>(T::widen(row.x[e]), e));
   }
-  constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;
-  for (int64_t b = int64_t(blockIdx.y) * kStep; b < row.vectors; b += int64_t(gridDim.y) * kStep) {
+  for (int64_t b = first; b < row.vectors; b += by) {
     uint32x4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -412,9 +452,27 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(Logprob
       float f[N];
       widen<T>(v[u], f);
 #pragma unroll
-      for (int k = 0; k < N; ++k) f[k] = r.at(f[k], i * N + k);
+      for (int k = 0; k < N; ++k) f[k] = r.template at<FAR>(f[k], i * N + k);
       store16(out + i * N, narrow<T>(f));
     }
+  }
+}
+
+// The workgroups of a row (blockIdx.y) take kUnroll vectors a thread of it in turn. A far
+// row is the first one's alone, which reads it twice: the gradient may lie on the logits.
+template <class T>
+__global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(LogprobGradArgs a) {
+  constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;
+  const int64_t t = blockIdx.x;
+  const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
+  typename T::raw* out = static_cast<typename T::raw*>(a.grad) + t * a.ldg;
+  GradRow r(a, t);
+  if (r.far) {
+    if (blockIdx.y != 0) return;
+    largest_and_log_sum<T>(row, r.m, r.log_s);
+    write_gradient<T, true>(row, r, out, 0, kStep);
+  } else {
+    write_gradient<T, false>(row, r, out, int64_t(blockIdx.y) * kStep, int64_t(gridDim.y) * kStep);
   }
 }
 
