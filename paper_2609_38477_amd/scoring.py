@@ -4,7 +4,8 @@ the head they were made from; the measured counterpart of the data-free gradient
 size; and single-bit faults of the 4-bit form.
 
 * ``score`` takes logits and the tokens that came next: mean negative log
-  likelihood, perplexity and entropy, and the likeliest tokens.
+  likelihood, perplexity and entropy, and the likeliest tokens. Rows with a negative
+  token (padding, a prompt) are in no mean.
 * The head in 4 bits gives its logits straight from the codes (``q4_gemv``), the
   seed-coded head from its decoded weights.
 * ``measured_rho`` is the gradient size at the head's input that the data itself
@@ -32,21 +33,24 @@ from . import (Q4Weights, footprint, q4_dequantize, q4_gemv, q4_quantize, token_
 
 
 def score(logits, tokens, top: int = 5) -> dict:
-    """Figures of logits [n, vocab] against the tokens [n] that came next."""
+    """Figures of logits [n, vocab] against the tokens [n] that came next, means over the
+    rows whose token is not negative (NaN if there is none)."""
     s = token_logprobs(logits, tokens, top=top)
-    nll = -s.logprob.double().mean().item()
-    return {"nll": nll, "perplexity": math.exp(nll) if nll < 700 else math.inf,
-            "entropy": s.entropy.double().mean().item(), "top": s.top_token}
+    asked = tokens >= 0
+    nll = -s.logprob[asked].double().mean().item()
+    return {"nll": nll, "perplexity": math.inf if nll >= 700 else math.exp(nll),   # NaN stays NaN
+            "entropy": s.entropy[asked].double().mean().item(), "top": s.top_token}
 
 
 def measured_rho(W, logits, tokens):
-    """rho (fp64 [d]) of the head W (fp32 [vocab, d]) on these logits and tokens."""
+    """rho (fp64 [d]) of the head W (fp32 [vocab, d]) on these logits and tokens, the mean
+    over the rows whose token is not negative (NaN if there is none)."""
     import torch
     from .frontend import sq_gemv
     s = token_logprobs(logits, tokens)
     minus = torch.full_like(s.lse, -1.0)
-    g = token_logprobs_backward(logits, tokens, s.lse, grad_logprob=minus)
-    return sq_gemv(W, (g.float() ** 2).mean(0), transpose=True)
+    g = token_logprobs_backward(logits, tokens, s.lse, grad_logprob=minus)   # 0 in the other rows
+    return sq_gemv(W, (g.float() ** 2).sum(0) / (tokens >= 0).sum(), transpose=True)
 
 
 def next_token(q: Q4Weights, h, top: int = 5):
@@ -78,9 +82,13 @@ def flip_bit(q: Q4Weights, part: str, index: int, bit: int) -> Q4Weights:
 
 
 def fault_study(q: Q4Weights, h, tokens) -> list:
-    """Footprint and negative log likelihood of one fault of every kind, in the row of tokens[0]."""
+    """Footprint and negative log likelihood of one fault of every kind, in the row of the
+    first token that is one."""
+    some = tokens[(tokens >= 0) & (tokens < q.nrows)]
+    if some.numel() == 0:
+        raise ValueError("tokens: none of them is one of the head's")
     clean = q4_dequantize(q)
-    row = int(tokens[0].item())
+    row = int(some[0].item())
     words, groups = q.codes.shape[1], q.scale.shape[1]
     kinds = [("lowest bit of a code", "codes", row * words, 0),
              ("highest bit of a code", "codes", row * words, 3),
