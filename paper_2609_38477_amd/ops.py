@@ -20,6 +20,7 @@ from . import lib as _base_lib
 
 SEEDQ_F32, SEEDQ_F16, SEEDQ_BF16 = 0, 1, 2
 SEEDQ_MAX_TOP = 32
+SEEDQ_EUNSUPPORTED = -2
 GROUPS = (32, 64, 128, 256, 512)
 
 _lib = None
@@ -196,6 +197,8 @@ def _check_q4(q: Q4Weights) -> int:
     """The device of q, whose tensors are what its sizes say."""
     import torch
     codes, zero = q.codes, q.zero
+    if q.group not in GROUPS:
+        _check(SEEDQ_EUNSUPPORTED, f"Q4Weights: group {q.group}")
     device = _device(codes, "codes")
     groups = (q.nrows, -(-q.ncols // q.group))
     _same(codes, device, (q.nrows, 4 * ((q.ncols + 31) // 32)), torch.int32, "codes")

@@ -23,3 +23,13 @@ def test_logprobs_workspace_covers_the_last_launch(sq, vocab, top, left):
     for launches in (1, 3):
         assert sq.seedq_token_logprobs_workspace_bytes((launches << 21) + left, vocab, top) == alone
         assert sq.seedq_token_logprobs_workspace_bytes(launches << 21, vocab, top) == 0
+
+
+@pytest.mark.parametrize("group", [0, -32, 16, 48, 1024])
+def test_coded_weights_of_no_group_size(sq, group):
+    import torch
+    q = sq.Q4Weights(torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, 2).half(), None, 4, 64, group)
+    for call in (lambda: sq.q4_dequantize(q), lambda: sq.q4_gemv(q, torch.zeros(2, 64))):
+        with pytest.raises(sq.SeedqError) as e:
+            call()
+        assert e.value.code == -2
