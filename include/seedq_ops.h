@@ -133,7 +133,8 @@ int seedq_token_logprobs(const void* d_logits, int32_t type, int64_t ld, int64_t
  * the row's own m and S, at the price of a second pass over it. p is 0 at -inf (the
  * gradient there is g at the token itself, else 0). A row without any finite logit (lse -inf) has gradient 0;
  * a NaN lse gives NaN. A negative token has no log probability to differentiate; one
- * >= vocab gives a NaN row.
+ * >= vocab gives a NaN row, without a finite logit too. Without g the tokens play no
+ * part.
  *   d_grad_logprob (g), d_grad_entropy (h): fp32 [nrows], at least one not NULL;
  *   d_grad_logprob needs d_tokens, d_grad_entropy needs d_entropy.
  *   d_grad_logits: type [nrows][vocab], row stride ldg >= vocab elements; nothing

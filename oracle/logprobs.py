@@ -33,10 +33,10 @@ def gradient(x, token, lse, entropy, g, h):
     """d(g logprob + h entropy) / dx of one row, with p = e^(x - lse)."""
     x = np.asarray(x, dtype=np.float64)
     V = x.size
-    if lse == -np.inf:
-        return np.zeros(V)
     if np.isnan(lse) or token >= V:
         return np.full(V, np.nan)
+    if lse == -np.inf:
+        return np.zeros(V)
     g = g if token >= 0 else 0.0
     d = np.zeros(V)
     for v in range(V):

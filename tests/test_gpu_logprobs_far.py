@@ -93,3 +93,17 @@ def test_a_fully_masked_row_is_uniform(sq, torch, dtype):
     d = sq.token_logprobs_backward(x, tokens, r.lse, grad_logprob=torch.ones(2, device="cuda")).float()
     assert abs(d[0, 3].item() - 0.999) < 2 ** -8 and abs(d[0, 4].item() + 0.001) < 1e-5
     assert (d.sum(1).abs() < 5e-3).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_token_outside_an_empty_row(sq, torch, dtype):
+    # with a gradient at its log probability NaN, as the log probability itself is; without, 0
+    x = torch.full((2, 300), -INF, dtype=getattr(torch, dtype), device="cuda")
+    tokens = torch.tensor([300, 5], device="cuda")
+    one = torch.ones(2, device="cuda")
+    r = sq.token_logprobs(x, tokens)
+    assert np.isnan(r.logprob[0].item()) and r.logprob[1].item() == -INF
+    d = sq.token_logprobs_backward(x, tokens, r.lse, r.entropy, one, one)
+    assert d[0].isnan().all() and not d[1].any()
+    d = sq.token_logprobs_backward(x, tokens, r.lse, r.entropy, None, one)
+    assert not d.any()

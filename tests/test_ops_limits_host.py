@@ -33,3 +33,11 @@ def test_coded_weights_of_no_group_size(sq, group):
         with pytest.raises(sq.SeedqError) as e:
             call()
         assert e.value.code == -2
+
+
+def test_oracle_gradient_of_a_token_outside_an_empty_row():
+    import numpy as np
+    from oracle import logprobs as olp
+    x = [-np.inf, -np.inf]
+    assert np.isnan(olp.gradient(x, 2, -np.inf, 0.0, 1.0, 0.5)).all()
+    assert not olp.gradient(x, 1, -np.inf, 0.0, 0.0, 0.5).any()
