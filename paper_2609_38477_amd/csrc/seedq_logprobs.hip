@@ -3,8 +3,9 @@
 //
 // Both are one pass over the logits in 16-byte vectors, bound by memory. Forward, each
 // thread keeps a running maximum m and, relative to it, S = sum e^(x - m) and
-// E = sum e^(x - m) (x - m); a larger maximum rescales both. The threads' sums meet in
-// fp64. The entropy log S - E / S adds two terms of one sign.
+// E = sum e^(x - m) (x - m) in fp32; a larger maximum rescales both. The threads' sums meet
+// in fp64, weighted by e^ of their maxima's distance in fp32, which errs by 2^-24 of the
+// distance like every term. The entropy log S - E / S adds two terms of one sign.
 #include <algorithm>
 #include <cfloat>
 
@@ -154,7 +155,7 @@ __device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
 // vectors lie in as many cache lines, which is what the second look costs: 2048 rows of
 // 131072 bf16 logits take 109 us with 5 alternatives, 118 with 20 and 110 with none. For
 // few rows the launch spends its time on the way through the code, so that is kept short:
-// one row of 32000 fp32 logits takes 5.9 us without alternatives and 9.0 with 20.
+// one row of 32000 fp32 logits takes 5.7 us without alternatives and 8.7 with 20.
 template <class T, int NT>
 __global__ void __launch_bounds__(NT)
 logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
@@ -460,6 +461,8 @@ __device__ __forceinline__ void write_gradient(const Row<T>& row, const GradRow&
 
 // The workgroups of a row (blockIdx.y) take kUnroll vectors a thread of it in turn. A far
 // row is the first one's alone, which reads it twice: the gradient may lie on the logits.
+// 4096 x 32000 bf16 takes 110 us, with far rows only 141, in fp32 212 and 297; a single far
+// row of 131072 59 us, where an ordinary one takes 3.3.
 template <class T>
 __global__ void __launch_bounds__(kGradThreads) logprobs_backward_kernel(LogprobGradArgs a) {
   constexpr int64_t kStep = int64_t(kUnroll) * kGradThreads;

@@ -5,7 +5,7 @@
 // row, so every group (32 to 512 columns) lies in 4 to 64 neighbouring lanes of
 // one wave and its extremes are found without LDS. At 8192 x 28672 bf16 in groups of 128 the
 // quantiser takes 129 us (4.6 TB/s) and the decoder 109 us (5.4 TB/s, the rate of a large
-// copy); at 4096 x 14336 fp32 47 us (5.7 TB/s, from the last-level cache in part) and 57 us.
+// copy); at 4096 x 14336 fp32 47 us (5.7 TB/s, from the last-level cache in part) and 55 us.
 // What is left over the copy's rate in 16 bits is the arithmetic, some 12 operations a
 // weight, more with zero points: 4096 x 14336 bf16 in groups of 64 takes 41 us with them.
 #include "seedq_ops_device.h"

@@ -162,8 +162,8 @@ __device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v)
 // steps of its own. Order of the sums: the columns of a lane and step, the steps, the
 // lanes as a tree, the slices in order.
 // Memory bounds one vector (8192 x 28672 fp16 27 to 31 us, 4.0 to 4.4 TB/s of codes and
-// scales), the vector ALU more: two take 34 us, four in fp32 58, of which half an
-// operation a product. 4096 x 4096 takes 5.0 us, 1.9 of them an empty launch.
+// scales), the vector ALU more: two take 34 to 38 us, four in fp32 57 to 59, of which half
+// an operation a product. 4096 x 4096 takes 5.0 to 5.7 us, 1.9 of them an empty launch.
 constexpr int kMaxWaves = 16;
 constexpr int kStepCols = 64 * 4 * kC;
 constexpr int kPanelBytes = 128 << 10;
@@ -322,9 +322,9 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
 // its columns in blocks of BC chunks and add their sums through LDS in order. A block has
 // SB scales a row, which a lane reads at once; its codes are read while the block before
 // is multiplied, x a chunk ahead.
-// 8192 x 28672 and 8 fp16 vectors take 42 to 45 us (2.9 TB/s of codes). Loads are answered in
-// order, so those of x wait behind the next block's codes: without them it takes 36, without
-// decoding as well 26, which is the memory's. The vectors laid out in LDS instead, for a
+// 8192 x 28672 and 8 fp16 vectors take 39 to 45 us (up to 3.1 TB/s of codes). Loads are
+// answered in order, so those of x wait behind the next block's codes: where the whole took
+// 45 us, it took 36 without them and 26 without decoding as well, which is the memory's. The vectors laid out in LDS instead, for a
 // split of the columns each, and the splits joined: 43 to 48 us, at 4096 x 4096 twice as long.
 constexpr int kBatchWaves = 8;
 
@@ -470,12 +470,15 @@ gemv_batch_kernel(Q4 q, int nvec, const uint16_t* __restrict__ x, int64_t ldx, v
 // 64; product t takes everybody's word t, or, where a group is 32 columns, words that
 // have changed lanes so that each half of the chunk has two products of its own.
 // Each group's product meets its scale, zero point and sum of x in fp32.
-// 32000 x 4096 and 512 vectors: 163 us in fp16, 172 to 177 in bf16 (820 and 760 to 780
-// TFLOP/s), where a library product of 16-bit matrices of that kind reaches 1130. In bf16,
-// without the loads of codes the rest takes 144, without
-// decoding or the scales 175, without the barriers or the loads to LDS 173; a second
-// stage ahead (three buffers) 190, 16x16x32 products, whose lanes read 64 bytes of a row,
-// 262 (their registers spill).
+// 32000 x 4096 and 512 vectors: 159 to 163 us in fp16, 169 to 184 in bf16 (840 and 790
+// TFLOP/s at best), where a library product of the decoded 16-bit matrix takes 100 after 65
+// of decoding, and of 2048 vectors 362 after 63 (the codes 660). The scale step is 64
+// operations of a wave a group, 128 in bf16, and comes oftener in smaller groups: 64 columns
+// take 207 us (229 with zero points), 32 columns 272 (382). In fp32, three products for one,
+// 425, in groups of 32 795. What bounds groups of 128 in bf16 is the loads of codes: without
+// them the rest took 144 of 172 us, while without decoding or the scales it took 175 and
+// without the barriers or the loads to LDS 173. A second stage ahead (three buffers) took
+// 190, 16x16x32 products, whose lanes read 64 bytes of a row, 262 (their registers spill).
 constexpr int kStage = 128;            // columns
 constexpr int kFragBytes = 1024;       // 64 lanes x 16
 constexpr int kStageFrags = 8;         // a stage of 32 vectors, each piece of x
@@ -731,8 +734,8 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   p.mt = nvec <= 32 ? 1 : 2;
   p.vec_tiles = int((nvec + 32 * p.mt - 1) / (32 * p.mt));
   // 64 rows a wave need as many tiles as the chip holds workgroups: 32000 x 4096 and 512
-  // vectors 172 us (32 rows: 181), in fp32 470 (636); 4096 x 4096 and 64 22.2 (18.2),
-  // 12000 x 1504 and 300 36.9 (29.8).
+  // vectors 169 us (32 rows: 173), in fp32 424 (481); 12000 x 1504 and 300 38.0 (30.1), in
+  // fp32 68.5 (58.9), 4096 x 4096 and 64 no difference.
   p.rt = (nrows + 255) / 256 * p.vec_tiles >= 512 ? 2 : 1;
   p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
   p.stages = (ncols + kStage - 1) / kStage;
@@ -741,7 +744,8 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   // Workgroups for two on each CU, of four stages at least (two in fp32, whose stages take
   // three times the products); each split more is more to join. 8192 x 28672 and 32
   // vectors: up to 512 workgroups 52.2 us, 256 74.4, 1024 56.6; 2000 x 8192 and 17: four
-  // stages 16.6, two 19.6; 1001 x 2056 and 100 in fp32: 24.9 and 21.1.
+  // stages 16.2, two 20.0; 1001 x 2056 and 100 in fp32: 25.2 and 22.0, but 4096 x 4096 and
+  // 64 in fp32 25.2 and 29.2.
   p.splits = int(std::max<int64_t>(
       1, std::min<int64_t>({512 / tiles, p.stages / (pieces == 3 ? 2 : 4), 32})));
   p.frag_bytes = align256(size_t(p.padded / kTileVecs) * p.stages * pieces * kStageFrags * kFragBytes);
@@ -797,8 +801,12 @@ hipError_t launch_gemm(const Q4& q, int64_t nvec, const void* d_x, int64_t ldx, 
 }
 
 // The ways: the vector ALU, 16x16x32 products, the tiles for many vectors. In fp32 the
-// first takes up to four vectors at a time, twice where the codes are few (4096 x 4096
-// and 8 vectors 16.9 us, the tiles 18.9; 32000 x 4096 and 4 36 and 34, and 8 72 and 35).
+// first takes up to four vectors at a time (14336 x 4096 and 4 19.6 us, the tiles 21.9; at
+// worst 8192 x 28672 and 4 56.7 and 53.8), twice where the codes are few (4096 x 4096 and
+// 5 13.1 and 16.6, and 8 16.5 and 16.2; 8192 x 4096 and 5 19.4 and 17.4). In 16 bits it
+// takes two, which a batch would do in less where the codes are many (8192 x 28672 in bf16
+// 38 and 33 us, 14336 x 4096 14.3 and 13.8), and the batch 16 (32000 x 4096 29.2 us, the
+// tiles 27.8; 4096 x 4096 8.1 and 13.7).
 enum class Way { kFew, kBatch, kMany };
 Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   if (xtype == SEEDQ_F32)

@@ -5,8 +5,10 @@ gradient.
 Every function of the C ABI has a wrapper of the same name that only marshals
 arguments. The helpers (``q4_quantize``, ``q4_dequantize``, ``q4_gemv``,
 ``token_logprobs``, ``token_logprobs_backward``) check their tensors, allocate the
-outputs and the workspace and call the wrappers; with ``stream`` given they
-allocate on that stream too. All of them are in the package's own namespace.
+outputs and the workspace and call the same functions directly; with ``stream``
+given they allocate on that stream too. All of them are in the package's own
+namespace. They stand outside autograd: a result carries no gradient, whatever its
+inputs ask for, and ``token_logprobs_backward`` is called by whoever wants one.
 """
 from __future__ import annotations
 
