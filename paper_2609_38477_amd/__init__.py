@@ -637,3 +637,9 @@ from .ops import (Q4Weights, TokenLogprobs, q4_dequantize, q4_gemv, q4_quantize,
                   seedq_q4_quantize, seedq_q4_row_words, seedq_token_logprobs,
                   seedq_token_logprobs_backward, seedq_token_logprobs_workspace_bytes,
                   token_logprobs, token_logprobs_backward)
+from .mx4 import (Mx4Weights, mx4_dequantize, mx4_gemv, mx4_matmul, mx4_quantize,  # noqa: E402,F401
+                  seedq_mx4_dequantize, seedq_mx4_gemv, seedq_mx4_gemv_workspace_bytes,
+                  seedq_mx4_matmul, seedq_mx4_matmul_workspace_bytes, seedq_mx4_quantize,
+                  seedq_mx4_row_words)
+from .beam import (BeamState, BeamStep, beam_reorder, beam_select, seedq_beam_reorder,  # noqa: E402,F401
+                   seedq_beam_select, seedq_beam_select_workspace_bytes)

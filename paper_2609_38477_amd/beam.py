@@ -1,0 +1,229 @@
+"""Beam search over the logits of a head (C ABI in ``include/seedq_beam.h``): one step's
+selection over beams and vocabulary, and the beams' states moved to those that continue
+them.
+
+Every function of the C ABI has a wrapper of the same name that only marshals
+arguments. The helpers (``beam_select``, ``beam_reorder``) check their tensors, allocate
+the outputs and the workspace and call the same functions directly; with ``stream``
+given they allocate on that stream too. All of them are in the package's own
+namespace. They stand outside autograd.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from dataclasses import dataclass
+
+from . import _check, _ptr, _stream
+from . import lib as _base_lib
+from .ops import _handle, _logits, _on, _rows, _same
+
+SEEDQ_MAX_BEAMS = 32
+SEEDQ_MAX_BEAM_TOP = 32
+SEEDQ_MAX_BEAM_STATES = 4096
+
+_lib = None
+
+
+class BeamState(ctypes.Structure):
+    _fields_ = [("d_src", ctypes.c_void_p), ("d_dst", ctypes.c_void_p), ("src_row", ctypes.c_int64),
+                ("dst_row", ctypes.c_int64), ("src_outer", ctypes.c_int64),
+                ("dst_outer", ctypes.c_int64), ("outer", ctypes.c_int64), ("inner", ctypes.c_int64)]
+
+
+def lib() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        L = _base_lib()
+        vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        L.seedq_beam_select_workspace_bytes.restype = sz
+        L.seedq_beam_select_workspace_bytes.argtypes = [i64, i32, i64, i32]
+        L.seedq_beam_select.restype = ctypes.c_int
+        L.seedq_beam_select.argtypes = [vp, i32, i64, i64, i32, i64, vp, vp, i64, i32, vp, vp, vp, vp, sz,
+                                        vp]
+        L.seedq_beam_reorder.restype = ctypes.c_int
+        L.seedq_beam_reorder.argtypes = [vp, i64, vp, i64, i32, i32, vp]
+        _lib = L
+    return _lib
+
+
+# ---------------------------------------------------------------- C ABI wrappers
+
+def seedq_beam_select_workspace_bytes(batch: int, beams: int, vocab: int, top: int) -> int:
+    return int(lib().seedq_beam_select_workspace_bytes(batch, beams, vocab, top))
+
+
+def seedq_beam_select(d_logits, type: int, ld: int, batch: int, beams: int, vocab: int, d_scores,
+                      d_finished, pad_token: int, top: int, d_score, d_parent, d_token,
+                      d_workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().seedq_beam_select(_ptr(d_logits), type, ld, batch, beams, vocab, _ptr(d_scores),
+                                   _ptr(d_finished), pad_token, top, _ptr(d_score), _ptr(d_parent),
+                                   _ptr(d_token), _ptr(d_workspace), workspace_bytes,
+                                   _stream(stream)), "seedq_beam_select")
+
+
+def seedq_beam_reorder(states, nstates: int, d_parent, batch: int, in_beams: int, out_beams: int,
+                       stream=None) -> None:
+    """states: a ctypes array of BeamState."""
+    _check(lib().seedq_beam_reorder(states, nstates, _ptr(d_parent), batch, in_beams, out_beams,
+                                    _stream(stream)), "seedq_beam_reorder")
+
+
+# ---------------------------------------------------------------- helpers
+
+_select_workspace = functools.lru_cache(maxsize=256)(seedq_beam_select_workspace_bytes)
+
+
+@dataclass
+class BeamStep:
+    """The continuations of ``beam_select``, [batch, top] each, the best first: score
+    fp32, parent (the beam in its sequence) and token int64. Where there are none left
+    score is -inf, parent and token -1."""
+    score: object
+    parent: object
+    token: object
+
+
+def beam_select(logits, scores, top: int, finished=None, pad_token: int = 0, stream=None) -> BeamStep:
+    """The ``top`` best continuations of each sequence over its beams and the
+    vocabulary: logits (torch fp32, fp16 or bf16 [batch * beams, vocab] on the GPU),
+    scores fp32 [batch, beams] (the log probabilities so far, -inf for a dead beam).
+    A beam that is ``finished`` (bool or uint8 [batch, beams]) is continued by pad_token
+    alone, at its own score."""
+    import torch
+    t, device = _logits(logits, "logits")
+    if scores.dim() != 2 or scores.shape[1] < 1 or scores.shape[1] > SEEDQ_MAX_BEAMS:
+        raise ValueError(f"scores: [batch, 1 to {SEEDQ_MAX_BEAMS} beams] wanted, not {tuple(scores.shape)}")
+    batch, beams = scores.shape
+    nrows, vocab = logits.shape
+    if nrows != batch * beams:
+        raise ValueError(f"logits: {batch * beams} rows wanted, not {nrows}")
+    if not 1 <= top <= SEEDQ_MAX_BEAM_TOP:
+        raise ValueError(f"top: 1 to {SEEDQ_MAX_BEAM_TOP} wanted, not {top}")
+    _same(scores, device, (batch, beams), torch.float32, "scores")
+    if finished is not None:
+        if finished.dtype != torch.bool:
+            _same(finished, device, (batch, beams), torch.uint8, "finished")
+        else:
+            _same(finished, device, (batch, beams), torch.bool, "finished")
+        if pad_token < 0:
+            raise ValueError(f"pad_token: not negative wanted, not {pad_token}")
+    with _on(stream):
+        x, ld = _rows(logits)
+        score = x.new_empty((batch, top), dtype=torch.float32)
+        parent, token = x.new_empty((2, batch, top), dtype=torch.int64).unbind(0)
+        nws = _select_workspace(batch, beams, vocab, top)
+        ws = x.new_empty(nws, dtype=torch.uint8) if nws else None
+        _check(lib().seedq_beam_select(x.data_ptr(), t, ld, batch, beams, vocab, scores.data_ptr(),
+                                       _ptr(finished), pad_token, top, score.data_ptr(),
+                                       parent.data_ptr(), token.data_ptr(), _ptr(ws), nws,
+                                       _handle(device)), "seedq_beam_select")
+    return BeamStep(score, parent, token)
+
+
+def _pieces(t):
+    """(row stride, pieces, stride of pieces, bytes of a piece) of the rows of t in bytes,
+    or None where a row is more than pieces at one stride."""
+    size = t.element_size()
+    inner, outer, step, i = size, 1, 0, t.dim() - 1
+    shape, stride = t.shape, t.stride()
+    while i > 0 and (shape[i] == 1 or stride[i] * size == inner):
+        inner *= shape[i]
+        i -= 1
+    while i > 0:
+        if shape[i] != 1:
+            at = stride[i] * size
+            if outer == 1:
+                if at < inner:
+                    return None
+                step = at
+            elif at != outer * step:
+                return None
+            outer *= shape[i]
+        i -= 1
+    return stride[0] * size, outer, step, inner
+
+
+def beam_reorder(states, parents, out=None, stream=None):
+    """The states of the beams that continue: row (i, j) of each result is row
+    (i, parents[i, j]) of its tensor, zeros for a parent that is none of the sequence's.
+
+    states: a tensor or a list of tensors of any type on the GPU, [batch * beams, ...]
+    each with the same number of rows; a row may be a part of a larger cache (a view).
+    parents: int64 [batch, out_beams]. ``out``: tensors of the results' shapes and the
+    states' types, or the states themselves, whose rows are then moved in place (those
+    that are their own parents stay untouched). Returns a tensor or a list like states."""
+    import torch
+    single = isinstance(states, torch.Tensor)
+    states = [states] if single else list(states)
+    if parents.dim() != 2 or not 1 <= parents.shape[1] <= SEEDQ_MAX_BEAMS:
+        raise ValueError(f"parents: [batch, 1 to {SEEDQ_MAX_BEAMS}] wanted, not {tuple(parents.shape)}")
+    if len(states) > SEEDQ_MAX_BEAM_STATES:
+        raise ValueError(f"states: {SEEDQ_MAX_BEAM_STATES} at the most, not {len(states)}")
+    batch, out_beams = parents.shape
+    device = parents.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"parents: on {parents.device}, not on the current GPU")
+    _same(parents, device, (batch, out_beams), torch.int64, "parents")
+    if out is not None:
+        out = [out] if isinstance(out, torch.Tensor) else list(out)
+        if len(out) != len(states):
+            raise ValueError(f"out: {len(states)} tensors wanted, not {len(out)}")
+    beams = None
+    with _on(stream):
+        results, keep = [], []
+        array = (BeamState * len(states))()
+        for k, s in enumerate(states):
+            if s.dim() < 1 or s.get_device() != device:
+                raise ValueError(f"states: tensors of rows on GPU {device} wanted, not "
+                                 f"{tuple(s.shape)} on {s.device}")
+            rows = s.shape[0]
+            if beams is None:
+                beams = rows // batch if batch else 1
+            if rows != batch * beams or not 1 <= beams <= SEEDQ_MAX_BEAMS:
+                raise ValueError(f"states: rows of {batch} sequences of 1 to {SEEDQ_MAX_BEAMS} beams "
+                                 f"wanted, not {rows}")
+            shape = (batch * out_beams, *s.shape[1:])
+            if out is None:
+                o = s.new_empty(shape)
+            else:
+                o = out[k]
+                if o.dtype != s.dtype or o.shape != shape or o.get_device() != device:
+                    raise ValueError(f"out: {s.dtype} of shape {shape} on GPU {device} wanted, not "
+                                     f"{o.dtype} {tuple(o.shape)} on {o.device}")
+            results.append(o)
+            if s.numel() == 0 or o.numel() == 0:
+                continue
+            src, dst = _pieces(s), _pieces(o)
+            if dst is None:
+                raise ValueError("out: rows that are pieces at one stride wanted")
+            if o.data_ptr() == s.data_ptr() and (src != dst or out_beams != beams):
+                raise ValueError("out: in place, the states' own layout and number of beams wanted")
+            if src is None or (src[1], src[3]) != (dst[1], dst[3]):
+                if out is not None and src is not None:
+                    src, dst = _split(src, dst)
+                else:
+                    s = s.contiguous()
+                    keep.append(s)
+                    src = _pieces(s)
+                    src, dst = _split(src, dst)
+            if src is None:
+                raise ValueError("out: pieces that divide the states' or are divided by them wanted")
+            array[k] = BeamState(s.data_ptr(), o.data_ptr(), src[0], dst[0], src[2], dst[2], src[1],
+                                 src[3])
+        _check(lib().seedq_beam_reorder(array, len(states), parents.data_ptr(), batch, beams or 1,
+                                        out_beams, _handle(device)), "seedq_beam_reorder")
+    return results[0] if single else results
+
+
+def _split(a, b):
+    """a and b with the pieces of the one whose pieces are longer cut to the other's."""
+    if a[3] < b[3]:
+        b, a = _split(b, a)
+        return a, b
+    row, outer, step, inner = a
+    if inner == b[3]:
+        return a, b
+    if inner % b[3] or (outer > 1 and step != inner):
+        return None, None
+    return (row, outer * (inner // b[3]), b[3], b[3]), b

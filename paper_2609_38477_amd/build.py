@@ -16,9 +16,10 @@ LIB_PATH = os.path.join(HERE, LIB_NAME)
 HIP_SOURCES = ["seedq_bases.hip", "seedq_search_mfma.hip", "seedq_compact.hip",
                "seedq_decompress.hip", "seedq_stream.hip",
                "seedq_footprint.hip", "seedq_frontend.hip", "seedq_noalloc.hip",
-               "seedq_q4.hip", "seedq_q4_gemv.hip", "seedq_logprobs.hip"]
+               "seedq_q4.hip", "seedq_q4_gemv.hip", "seedq_logprobs.hip", "seedq_mx4.hip",
+               "seedq_mx4_gemv.hip", "seedq_mx4_matmul.hip", "seedq_beam.hip"]
 HOST_SOURCES = ["seedq_api.cpp", "seedq_schedule.cpp", "seedq_frontend_host.cpp",
-                "seedq_ops_api.cpp"]
+                "seedq_ops_api.cpp", "seedq_mx4_api.cpp", "seedq_beam_api.cpp"]
 
 # Device code is compiled without packed fp32 instructions.
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

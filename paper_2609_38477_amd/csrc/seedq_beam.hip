@@ -1,0 +1,444 @@
+// One step of beam search: the selection over beams and vocabulary, and the states of the
+// beams moved to those that continue them.
+#include <algorithm>
+#include <cfloat>
+
+#include "seedq_beam_internal.h"
+#include "seedq_top.h"
+
+namespace seedq {
+namespace {
+
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kFar = -1e30f;      // stands in for x - m = -inf: its e^ is 0
+constexpr int kUnroll = 4;          // vectors in flight a thread
+constexpr int kMaxSegs = 16;
+constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
+static_assert(SEEDQ_MAX_BEAM_TOP <= kMaxTop, "the selection of a row");
+
+// ---------------------------------------------------------------- selection
+//
+// total(b, v) = s_b + (x_bv - m_b) - log S_b with m_b the largest logit of beam b and S_b =
+// sum e^(x - m_b). Within a beam the order is that of the logits, so no more than the `top`
+// largest of each row can be among a sequence's: the first kernel goes over the logits once
+// and leaves of every row, or segment of one, m, S and the keys of its largest elements,
+// the second ranks what the beams of a sequence offer. Totals of different beams may lie
+// next to each other, so each vector quartet's sum joins S in fp64.
+
+struct Partial {
+  double S;
+  float m, unused;
+};
+
+__device__ __forceinline__ bool offers_tokens(const BeamArgs& a, int64_t t) {
+  return !(a.finished && a.finished[t]) && a.scores[t] != -kInf;
+}
+
+// One workgroup of NT threads a row, or a segment of one (blockIdx.y of segs).
+template <class T, int NT>
+__global__ void __launch_bounds__(NT)
+beam_rows_kernel(BeamArgs a, uint32_t segs, uint32_t seg_vectors, Partial* __restrict__ partial,
+                 Key* __restrict__ seg_top) {
+  constexpr int N = kPerVector<T>, kWaves = NT / 64;
+  __shared__ double sd[kWaves];
+  __shared__ float sf[kWaves];
+  __shared__ Chosen<NT> chosen;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = blockIdx.y;
+  const int64_t t = blockIdx.x;
+  if (!offers_tokens(a, t)) return;
+  const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
+  const uint32_t begin = std::min(seg * seg_vectors, row.vectors);
+  const uint32_t end = std::min(begin + seg_vectors, row.vectors);
+  float m = -FLT_MAX, best = -kInf;
+  double S = 0.0;
+  uint32_t base = 0;
+  const auto raise = [&](float to) {
+    if (to > m) {
+      S *= double(__builtin_amdgcn_exp2f(fmaxf(m - to, kFar) * kLog2E));
+      m = to;
+    }
+  };
+  const auto term = [&](float x) {   // a NaN stays one: m is infinite only without a distribution
+    return __builtin_amdgcn_exp2f(__builtin_elementwise_maximum(x - m, kFar) * kLog2E);
+  };
+  const auto note = [&](float l, uint32_t at) {
+    if (l > best) {
+      best = l;
+      base = at;
+    }
+  };
+#pragma unroll 1
+  for (uint32_t i = begin; i < end; i += kUnroll * NT) {
+    uint32x4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      v[u] = minus_infinity<T>();   // adds nothing
+      if (i + u * NT + tid < end) v[u] = row.load(i + u * NT + tid);
+    }
+    float f[kUnroll][N], top = -kInf, sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      widen<T>(v[u], f[u]);
+      const float l = largest(f[u]);
+      note(l, (i + u * NT + tid) * N);
+      top = fmaxf(top, l);
+    }
+    raise(top);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (i + u * NT < end)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum += term(f[u][k]);
+    S += double(sum);
+  }
+  const uint32_t after = row.vectors * N;
+  const bool has_tail = seg == segs - 1 && tid < row.tail;   // elements after the last vector
+  if (has_tail) {
+    const float x = T::widen(row.x[after + tid]);
+    raise(x);
+    S += double(term(x));
+    note(x, after + tid);
+  }
+  const Key mine = best > -kInf ? order_key(best, base) : 0;
+  // the sums of the threads
+  float most = lanes_reduce(m, [](float p, float q) { return fmaxf(p, q); });
+  if (lane == 0) sf[wave] = most;
+  if (tid == 0) chosen.npicked = chosen.nfound = 0;
+  __syncthreads();
+  most = sf[0];
+  for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sf[w]);
+  S *= double(__builtin_amdgcn_exp2f(fmaxf(m - most, kFar) * kLog2E));
+  S = lanes_reduce(S, [](double p, double q) { return p + q; });
+  if (lane == 0) sd[wave] = S;
+  top_note<NT>(chosen, mine);
+  __syncthreads();
+  S = sd[0];
+  for (int w = 1; w < kWaves; ++w) S += sd[w];
+  const int64_t at = t * int64_t(segs) + seg;
+  if (tid == 0) partial[at] = Partial{S, most, 0.f};
+  auto put = [&](int rank, Key key) { seg_top[at * a.top + rank] = key; };
+  if (!(S > 0.0)) {   // nothing left, or no distribution (the same for all threads)
+    for (int k = int(tid); k < a.top; k += NT) put(k, 0);
+    return;
+  }
+  top_finish<T, NT>(chosen, row, begin, end, has_tail, seg == segs - 1, mine, a.top, put);
+}
+
+// What a sequence may be continued by, in falling order: (total, beam, key) as two numbers.
+struct Offer {
+  uint64_t total;   // monotone in the total; 0 for none
+  uint32_t beam;
+  Key key;
+  __device__ __forceinline__ bool before(const Offer& o) const {
+    if (total != o.total) return total > o.total;
+    return beam != o.beam ? beam < o.beam : key > o.key;
+  }
+};
+__device__ __forceinline__ uint64_t order_of(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);   // -0 is 0
+  return b >> 63 ? ~b : b | uint64_t(1) << 63;
+}
+__device__ __forceinline__ double total_of(uint64_t k) {
+  return __builtin_bit_cast(double, k >> 63 ? k & ~(uint64_t(1) << 63) : ~k);
+}
+
+// A workgroup a sequence. Its beams' segments are lists of offers in falling order. With as
+// many lists as continuations the top-th best of their first offers bounds what is ranked;
+// with fewer, the best of their last ones, or the worst of those so far down that there are
+// `top` in all.
+constexpr int kJoinThreads = 256;
+constexpr int kMaxLists = kMaxBeams * kMaxSegs;
+__global__ void __launch_bounds__(kJoinThreads)
+beam_join_kernel(BeamArgs a, int segs, const Partial* __restrict__ partial,
+                 const Key* __restrict__ seg_top) {
+  enum { kNone, kTokens, kFinished, kBad };
+  __shared__ double far[kMaxBeams];    // m + log S, and in two parts: m
+  __shared__ double log_s[kMaxBeams];
+  __shared__ float score[kMaxBeams];
+  __shared__ int kind[kMaxBeams], bad, n, any_bound;
+  __shared__ Offer list[kMaxTop * kMaxTop], bound, first[kMaxLists], last[kMaxTop];
+  const int tid = int(threadIdx.x);
+  const int64_t i = blockIdx.x, t0 = i * a.beams;
+  if (tid == 0) bad = n = any_bound = 0;
+  __syncthreads();
+  if (tid < a.beams) {
+    const int64_t t = t0 + tid;
+    const float s = a.scores[t];
+    int k = kNone;
+    if (!(s < kInf)) k = kBad;
+    else if (s > -kInf && a.finished && a.finished[t]) k = kFinished;
+    else if (s > -kInf) {
+      const Partial* p = partial + t * segs;
+      float m = p[0].m;
+      for (int g = 1; g < segs; ++g) m = fmaxf(m, p[g].m);
+      double S = 0.0;
+      for (int g = 0; g < segs; ++g)
+        S += double(__builtin_amdgcn_exp2f(fmaxf(p[g].m - m, kFar) * kLog2E)) * p[g].S;
+      far[tid] = m;
+      log_s[tid] = log(S);
+      k = S > 0.0 ? kTokens : S == 0.0 ? kNone : kBad;
+    }
+    score[tid] = s;
+    kind[tid] = k;
+    if (k == kBad) bad = 1;
+  }
+  __syncthreads();
+  const int64_t out = i * a.top;
+  if (bad) {
+    for (int r = tid; r < a.top; r += kJoinThreads) {
+      a.score[out + r] = __builtin_nanf("");
+      a.parent[out + r] = a.token[out + r] = -1;
+    }
+    return;
+  }
+  const int lists = a.beams * segs;
+  const auto offer = [&](int l, int pos) {
+    const uint32_t b = uint32_t(l / segs);
+    Offer o{0, b, 0};
+    if (kind[b] == kTokens) {
+      o.key = seg_top[(t0 * segs + l) * a.top + pos];
+      if (o.key) o.total = order_of(double(score[b]) + ((double(key_value(o.key)) - far[b]) - log_s[b]));
+    } else if (kind[b] == kFinished && l % segs == 0 && pos == 0) {
+      o.key = 1;
+      o.total = order_of(double(score[b]));
+    }
+    return o;
+  };
+  const bool many = lists >= a.top;
+  const int deep = many ? 0 : (a.top + lists - 1) / lists - 1;
+  for (int l = tid; l < lists; l += kJoinThreads) {
+    first[l] = offer(l, deep);
+    if (many) continue;
+    last[l] = offer(l, a.top - 1);
+    if (first[l].total == 0) any_bound = -1;   // the worst of them is none
+  }
+  __syncthreads();
+  if (many) {
+    for (int l = tid; l < lists; l += kJoinThreads) {
+      const Offer mine = first[l];
+      int rank = 0;
+      for (int j = 0; j < lists; ++j) rank += first[j].before(mine) ? 1 : 0;
+      if (rank == a.top - 1 && mine.total) {
+        bound = mine;
+        any_bound = 1;
+      }
+    }
+  } else if (tid == 0) {
+    Offer worst = first[0];
+    for (int l = 1; l < lists; ++l)
+      if (worst.before(first[l])) worst = first[l];
+    Offer lowest = worst;
+    bool some = any_bound == 0;
+    for (int l = 0; l < lists; ++l) {
+      if (last[l].total && (!some || last[l].before(lowest))) {
+        lowest = last[l];
+        some = true;
+      }
+    }
+    bound = lowest;
+    any_bound = some ? 1 : 0;
+  }
+  __syncthreads();
+  const bool cut = any_bound == 1;
+  for (int k = tid; k < lists * a.top; k += kJoinThreads) {
+    const int l = k / a.top;
+    if (many && cut && bound.before(first[l])) continue;   // the whole list lies below
+    const Offer o = offer(l, k % a.top);
+    if (o.total && !(cut && bound.before(o))) {
+      const int at = atomicAdd(&n, 1);
+      list[at] = o;
+    }
+  }
+  __syncthreads();
+  const int count = n;
+  for (int k = tid; k < count; k += kJoinThreads) {
+    const Offer mine = list[k];
+    int rank = 0;
+    for (int j = 0; j < count; ++j) rank += list[j].before(mine) ? 1 : 0;
+    if (rank >= a.top) continue;
+    a.score[out + rank] = float(total_of(mine.total));
+    a.parent[out + rank] = mine.beam;
+    a.token[out + rank] = kind[mine.beam] == kFinished ? a.pad_token : int64_t(key_index(mine.key));
+  }
+  for (int r = count + tid; r < a.top; r += kJoinThreads) {
+    a.score[out + r] = -kInf;
+    a.parent[out + r] = a.token[out + r] = -1;
+  }
+}
+
+// Segments of a row. The join is there in any case, so rows are cut where they are few.
+int segments(int64_t rows, int64_t vocab, int per_vector) {
+  const int64_t n = vocab / per_vector;
+  return int(std::max<int64_t>(1, std::min<int64_t>({n / 2048, 512 / rows, kMaxSegs})));
+}
+
+size_t partial_bytes(int64_t rows, int segs) { return align256(size_t(rows) * segs * sizeof(Partial)); }
+
+constexpr int64_t kMaxBatch = kMaxRows / kMaxBeams;   // sequences of one launch
+
+size_t rows_bytes(int64_t rows, int64_t vocab, int top) {
+  const int segs = segments(rows, vocab, 4);   // the type with the most
+  return partial_bytes(rows, segs) + align256(size_t(rows) * segs * top * sizeof(Key));
+}
+
+// ---------------------------------------------------------------- reordering
+
+// Units of 16 bytes of the pieces' lengths, the last of a piece shorter. A thread takes the
+// same unit of all rows of a sequence: it reads those of the parents, then writes, so that a
+// tensor can be its own destination, every parent's unit comes from memory once, and rows
+// that stay are left alone.
+struct State {
+  const char* src;
+  char* dst;
+  int64_t src_row, dst_row, src_outer, dst_outer, inner;
+  uint32_t per_piece, in_place;
+  uint32_t units;         // per_piece x outer
+  uint32_t first_block;   // of a sequence's
+};
+constexpr int kStates = 44;   // below 64
+struct States {
+  State s[kStates];
+  int n;
+};
+static_assert(sizeof(States) <= 3584, "fits the kernel's arguments");
+constexpr int kMoveThreads = 256;
+
+template <int NB>
+__global__ void __launch_bounds__(kMoveThreads)
+reorder_kernel(States all, const int64_t* __restrict__ parent, int in_beams, int out_beams) {
+  const int64_t seq = blockIdx.y;
+  int which = 0;   // the last whose first block is not past this one
+  for (int step = 32; step > 0; step >>= 1)
+    if (which + step < all.n && blockIdx.x >= all.s[which + step].first_block) which += step;
+  const State& s = all.s[which];
+  const uint32_t u = (blockIdx.x - s.first_block) * kMoveThreads + threadIdx.x;
+  if (u >= s.units) return;
+  const uint32_t piece = u / s.per_piece;
+  const int64_t at = int64_t(u - piece * s.per_piece) * 16;
+  const char* src = s.src + seq * in_beams * s.src_row + piece * s.src_outer + at;
+  char* dst = s.dst + seq * out_beams * s.dst_row + piece * s.dst_outer + at;
+  const int64_t* par = parent + seq * out_beams;
+  const int64_t left = s.inner - at;
+  const auto from = [&](int j) { return par[j] >= 0 && par[j] < in_beams ? par[j] : int64_t(-1); };
+  if (left >= 16) {
+    uint32x4 v[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      v[j] = uint32x4{0u, 0u, 0u, 0u};
+      if (j < out_beams) {
+        const int64_t p = from(j);
+        if (p >= 0 && !(s.in_place && p == j)) v[j] = load16(src + p * s.src_row);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (j < out_beams && !(s.in_place && par[j] == j)) store16(dst + j * s.dst_row, v[j]);
+  } else {
+    for (int64_t b = 0; b < left; ++b) {
+      char v[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        v[j] = 0;
+        if (j < out_beams && from(j) >= 0 && !(s.in_place && par[j] == j))
+          v[j] = src[from(j) * s.src_row + b];
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        if (j < out_beams && !(s.in_place && par[j] == j)) dst[j * s.dst_row + b] = v[j];
+    }
+  }
+}
+
+}  // namespace
+
+size_t beam_select_workspace_bytes(int64_t batch, int beams, int64_t vocab, int top) {
+  size_t need = rows_bytes(std::min(batch, kMaxBatch) * beams, vocab, top);
+  if (batch > kMaxBatch && batch % kMaxBatch)   // the last launch of many may cut its rows
+    need = std::max(need, rows_bytes(batch % kMaxBatch * beams, vocab, top));
+  return need;
+}
+
+hipError_t launch_beam_select(const BeamArgs& all, int type, void* d_ws, hipStream_t stream) {
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    for (int64_t b = 0; b < all.batch; b += kMaxBatch) {   // the launches share the workspace
+      BeamArgs a = all;
+      a.batch = std::min(kMaxBatch, all.batch - b);
+      a.logits = static_cast<const typename T::raw*>(all.logits) + b * a.beams * a.ld;
+      a.scores += b * a.beams;
+      if (a.finished) a.finished += b * a.beams;
+      a.score += b * a.top, a.parent += b * a.top, a.token += b * a.top;
+      const int64_t rows = a.batch * a.beams;
+      const int segs = segments(rows, a.vocab, kPerVector<T>);
+      Partial* part = static_cast<Partial*>(d_ws);
+      Key* keys = reinterpret_cast<Key*>(static_cast<char*>(d_ws) + partial_bytes(rows, segs));
+      const uint32_t n = uint32_t(a.vocab) / kPerVector<T>;
+      auto go = [&](auto kern, unsigned threads) {
+        hipLaunchKernelGGL(kern, dim3(unsigned(rows), unsigned(segs)), dim3(threads), 0, stream, a,
+                           uint32_t(segs), (n + segs - 1) / segs, part, keys);
+      };
+      if (n <= 256) go(beam_rows_kernel<T, 64>, 64);
+      else go(beam_rows_kernel<T, 512>, 512);
+      hipLaunchKernelGGL(beam_join_kernel, dim3(unsigned(a.batch)), dim3(kJoinThreads), 0, stream, a,
+                         segs, part, keys);
+    }
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_beam_reorder(const seedq_beam_state* states, int64_t nstates, const int64_t* d_parent,
+                               int64_t batch, int in_beams, int out_beams, hipStream_t stream) {
+  constexpr int64_t kMaxBlocks = int64_t(1) << 23;   // of a launch's grid
+  States all;
+  all.n = 0;
+  int64_t blocks = 0;
+  const auto flush = [&]() {
+    for (int64_t b = 0; b < batch && blocks; b += 65535) {
+      States part = all;
+      for (int i = 0; i < part.n; ++i) {
+        part.s[i].src += b * in_beams * part.s[i].src_row;
+        part.s[i].dst += b * out_beams * part.s[i].dst_row;
+      }
+      const dim3 grid(unsigned(blocks), unsigned(std::min<int64_t>(batch - b, 65535)));
+      auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, grid, dim3(kMoveThreads), 0, stream, part, d_parent + b * out_beams,
+                           in_beams, out_beams);
+      };
+      if (out_beams <= 4) go(reorder_kernel<4>);
+      else if (out_beams <= 8) go(reorder_kernel<8>);
+      else if (out_beams <= 16) go(reorder_kernel<16>);
+      else go(reorder_kernel<32>);
+    }
+    all.n = 0;
+    blocks = 0;
+  };
+  for (int64_t i = 0; i < nstates; ++i) {
+    const seedq_beam_state& s = states[i];
+    if (s.outer == 0 || s.inner == 0) continue;
+    State d{static_cast<const char*>(s.d_src), static_cast<char*>(s.d_dst), s.src_row, s.dst_row,
+            s.src_outer, s.dst_outer, s.inner, 0, s.d_src == s.d_dst ? 1u : 0u, 0, 0};
+    int64_t outer = s.outer;
+    // Pieces longer than 2^31 bytes, and rows of very many units, are cut.
+    for (int64_t o = 0; o < outer;) {
+      for (int64_t at = 0; at < s.inner;) {
+        const int64_t len = std::min<int64_t>(s.inner - at, int64_t(1) << 31);
+        const int64_t per = (len + 15) / 16;
+        const int64_t take = len < s.inner ? 1 : std::min<int64_t>(outer - o, std::max<int64_t>(1, (int64_t(1) << 27) / per));
+        State e = d;
+        e.src += o * s.src_outer + at, e.dst += o * s.dst_outer + at;
+        e.inner = len, e.per_piece = uint32_t(per), e.units = uint32_t(per * take);
+        const int64_t need = (int64_t(e.units) + kMoveThreads - 1) / kMoveThreads;
+        if (all.n == kStates || blocks + need > kMaxBlocks) flush();
+        e.first_block = uint32_t(blocks);
+        all.s[all.n++] = e;
+        blocks += need;
+        at += len;
+        if (at >= s.inner) o += take;
+      }
+    }
+  }
+  flush();
+  return hipGetLastError();
+}
+
+}  // namespace seedq

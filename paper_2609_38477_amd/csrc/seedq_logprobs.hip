@@ -9,51 +9,15 @@
 #include <algorithm>
 #include <cfloat>
 
-#include "seedq_ops_device.h"
+#include "seedq_top.h"
 
 namespace seedq {
 namespace {
 
-typedef unsigned long long Key;
-
-constexpr float kInf = __builtin_inff();
 constexpr float kLog2E = 1.44269504088896340736f;
 constexpr float kFar = -1e30f;      // stands in for x - m = -inf: its e^ is 0, and so is 0 x kFar
 constexpr int kUnroll = 4;          // vectors in flight a thread
-constexpr int kMaxTop = SEEDQ_MAX_TOP;
-constexpr int kManyPicked = 2 * kMaxTop;
 constexpr int kMaxSegs = 16;
-
-// Order of alternatives in one number: the value's pattern made monotonic (-0 is
-// 0), then the lower index first. 0 stands for none.
-__device__ __forceinline__ Key order_key(float x, uint32_t index) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
-  const uint32_t k = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return (Key(k) << 32) | (0xFFFFFFFFu - index);
-}
-__device__ __forceinline__ float key_value(Key key) {
-  const uint32_t k = uint32_t(key >> 32);
-  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
-}
-__device__ __forceinline__ uint32_t key_index(Key key) { return 0xFFFFFFFFu - uint32_t(key); }
-__device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
-
-// A row in 16-byte vectors and the elements after the last.
-template <class T>
-struct Row {
-  static constexpr int N = kPerVector<T>;
-  const typename T::raw* x;
-  uint32_t vectors, tail;   // a row has fewer than 2^31 elements
-  __device__ Row(const typename T::raw* p, int64_t n)
-      : x(p), vectors(uint32_t(n) / N), tail(uint32_t(n) % N) {}
-  __device__ __forceinline__ uint32x4 load(uint32_t i) const { return load16(x + size_t(i) * N); }
-};
-
-template <class T>
-__device__ __forceinline__ uint32x4 minus_infinity() {
-  const uint32_t w = kPerVector<T> == 4 ? 0xFF800000u : uint32_t(T::narrow(-kInf)) * 0x10001u;
-  return uint32x4{w, w, w, w};
-}
 
 struct Sums {
   float m = -FLT_MAX, S = 0.f, E = 0.f;
@@ -83,14 +47,6 @@ struct Sums {
     }
   }
 };
-
-template <int N>
-__device__ __forceinline__ float largest(const float (&f)[N]) {
-  float t = f[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) t = fmaxf(t, f[i]);
-  return t;
-}
 
 // What a segment of a row hands to the join.
 struct Partial {
@@ -130,43 +86,20 @@ __device__ __forceinline__ void write_alternative(const LogprobArgs& a, int64_t 
       bad ? __builtin_nanf("") : none ? -kInf : float((double(key_value(key)) - m) - log_s);
 }
 
-// The keys of list[0 .. n) in falling order: f(rank, key) for the first `top` ranks.
-template <class F>
-__device__ __forceinline__ void by_rank(const Key* list, int n, int top, F f) {
-  for (int i = int(threadIdx.x); i < n; i += int(blockDim.x)) {
-    const Key mine = list[i];
-    int rank = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
-    if (rank < top) f(rank, mine);
-  }
-}
-
 // One workgroup of NT threads a row, or a segment of one (blockIdx.y of segs), whose
 // sums and alternatives then go to the join.
-//
-// Alternatives: a thread remembers its largest element and the vector that first had it.
-// The top-th largest of the largest keys of 64 groups of threads bounds the top-th
-// largest element from below (where many keys reach it, as among equal logits, the
-// top-th largest key takes its place), so only the vectors of threads whose keys reach
-// the bound are read again, by all threads together, and the elements that reach it are
-// ranked against each other. Vectors are intervals of the row, so the order of (value,
-// first vector) is that of (value, index), and ties are cut the same way. A thread's
-// vectors lie in as many cache lines, which is what the second look costs: 2048 rows of
-// 131072 bf16 logits take 109 us with 5 alternatives, 118 with 20 and 110 with none. For
-// few rows the launch spends its time on the way through the code, so that is kept short:
-// one row of 32000 fp32 logits takes 5.7 us without alternatives and 8.7 with 20.
+// The second look at the likeliest costs as many cache lines as a thread has vectors: 2048
+// rows of 131072 bf16 logits take 109 us with 5 alternatives, 118 with 20 and 110 with
+// none. For few rows the launch spends its time on the way through the code, so that is
+// kept short: one row of 32000 fp32 logits takes 5.7 us without alternatives and 8.7 with 20.
 template <class T, int NT>
 __global__ void __launch_bounds__(NT)
 logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
                 Partial* __restrict__ partial, Key* __restrict__ seg_top) {
-  constexpr int N = kPerVector<T>, kWaves = NT / 64, kGroup = NT / 64;
-  constexpr int kPicked = kMaxTop * kGroup;        // the keys of kMaxTop groups
-  constexpr int kFound = NT == 64 ? 512 : 1024;    // elements kept before the slow selection
+  constexpr int N = kPerVector<T>, kWaves = NT / 64;
   __shared__ double sd[2][kWaves];
   __shared__ float sf[kWaves];
-  __shared__ Key group_key[64], picked[kPicked], found[kFound], tighter;
-  __shared__ int npicked, nfound;
+  __shared__ Chosen<NT> chosen;
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = blockIdx.y;
   const int64_t t = blockIdx.x;
   const Row<T> row(static_cast<const typename T::raw*>(a.logits) + t * a.ld, a.vocab);
@@ -211,7 +144,7 @@ logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
   // the sums of the threads
   float m = lanes_reduce(s.m, [](float p, float q) { return fmaxf(p, q); });
   if (lane == 0) sf[wave] = m;
-  if (tid == 0) npicked = nfound = 0;
+  if (tid == 0) chosen.npicked = chosen.nfound = 0;
   __syncthreads();
   m = sf[0];
   for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sf[w]);
@@ -224,8 +157,7 @@ logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
     sd[1][wave] = E;
   }
   // the largest element of each of 64 groups of threads
-  const Key g = lanes_reduce<kGroup>(mine, max_key);
-  if (tid % kGroup == 0) group_key[tid / kGroup] = g;
+  top_note<NT>(chosen, mine);
   __syncthreads();
   S = sd[0][0], E = sd[1][0];
   for (int w = 1; w < kWaves; ++w) {
@@ -247,76 +179,7 @@ logprobs_kernel(LogprobArgs a, uint32_t segs, uint32_t seg_vectors,
     for (int k = int(tid); k < a.top; k += NT) put(k, 0);
     return;
   }
-  Key bound;
-  {   // every wave for itself
-    const Key key = group_key[lane];
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < 64; ++j) rank += group_key[j] > key ? 1 : 0;
-    const unsigned long long cut = __ballot(rank == a.top - 1);
-    bound = cut ? max_key(__shfl(key, __builtin_ctzll(cut), 64), 1) : 1;   // fewer groups: all keys
-    if (mine >= bound) picked[atomicAdd(&npicked, 1)] = mine;
-  }
-  __syncthreads();
-  const int npick = npicked;
-  if (npick > kManyPicked) {
-    by_rank(picked, npick, a.top, [&](int rank, Key key) {
-      if (rank == a.top - 1) tighter = key;
-    });
-    __syncthreads();
-    bound = tighter;
-  }
-  auto take = [&](float x, uint32_t index, uint32_t base) {
-    if (x > -kInf && order_key(x, base) >= bound) {
-      const int k = atomicAdd(&nfound, 1);
-      if (k < kFound) found[k] = order_key(x, index);
-    }
-  };
-  // all threads over (picked key, the vectors of its thread)
-  const uint32_t each = (end - begin + NT - 1) / NT;
-#pragma unroll 1
-  for (uint32_t p = tid; p < uint32_t(npick) * each; p += NT) {
-    const uint32_t which = p / each;
-    const Key key = picked[which];
-    const uint32_t e = key_index(key);
-    const uint32_t owner = e < after ? (e / N - begin) % NT : e - after;
-    const uint32_t v = begin + owner + (p - which * each) * NT;
-    if (key < bound || v >= end) continue;
-    float f[N];
-    widen<T>(row.load(v), f);
-    if (order_key(largest(f), v * N) >= bound)
-#pragma unroll
-      for (int k = 0; k < N; ++k) take(f[k], v * N + k, v * N);
-  }
-  if (has_tail) take(T::widen(row.x[after + tid]), after + tid, after + tid);
-  __syncthreads();
-  const int n = nfound;
-  if (n <= kFound) {
-    by_rank(found, n, a.top, put);
-    for (int k = n + int(tid); k < a.top; k += NT) put(k, 0);
-    return;
-  }
-  // More elements reach the bound than are kept, as when a thread's elements are all
-  // among the largest: one pass over the segment for each alternative.
-  Key last = ~Key(0);
-  const uint32_t stop = seg == segs - 1 ? uint32_t(a.vocab) : end * N;
-#pragma unroll 1
-  for (int k = 0; k < a.top; ++k) {
-    Key best = 0;
-#pragma unroll 1
-    for (uint32_t e = begin * N + tid; e < stop; e += NT) {
-      const float x = T::widen(row.x[e]);
-      const Key key = order_key(x, e);
-      if (x > -kInf && key < last && key > best) best = key;
-    }
-    best = lanes_reduce(best, max_key);
-    __syncthreads();
-    if (lane == 0) picked[wave] = best;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) best = max_key(best, picked[w]);
-    if (tid == 0) put(k, best);
-    last = best ? best : 1;   // after the last one nothing is below
-  }
+  top_finish<T, NT>(chosen, row, begin, end, has_tail, seg == segs - 1, mine, a.top, put);
 }
 
 // The segments of a row: sums in the order of the segments, alternatives of all of them

@@ -1,28 +1,14 @@
 // C ABI entry points of seedq_ops.h: argument checks and launches.
-#include "seedq_ops_internal.h"
+#include "seedq_ops_checks.h"
 
 using namespace seedq;
 
 namespace {
 
-bool type_ok(int32_t t) { return t == SEEDQ_F32 || t == SEEDQ_F16 || t == SEEDQ_BF16; }
-uintptr_t type_size(int32_t t) { return t == SEEDQ_F32 ? 4 : 2; }
-
-bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-
-// Leading dimensions and counts below keep every byte offset far inside 63 bits.
-bool ld_ok(int64_t ld, int64_t n) { return ld >= n && ld <= (int64_t(1) << 40); }
-
 int group_shift(int32_t group) {
   for (int s = 5; s <= 9; ++s)
     if (group == 1 << s) return s;
   return 0;
-}
-
-bool shape_ok(int64_t nrows, int64_t ncols) {
-  if (nrows <= 0 || ncols <= 0 || ncols % kC != 0) return false;
-  const int64_t G = ncols / kC;
-  return nrows <= (int64_t(1) << 31) / G && nrows * G < (int64_t(1) << 31);
 }
 
 int q4_args(const uint32_t* d_codes, const void* d_scale, const uint8_t* d_zero, int64_t nrows,
@@ -35,8 +21,6 @@ int q4_args(const uint32_t* d_codes, const void* d_scale, const uint8_t* d_zero,
          q4_groups(ncols, group), gshift};
   return SEEDQ_OK;
 }
-
-int result(hipError_t e) { return e == hipSuccess ? SEEDQ_OK : SEEDQ_EHIP; }
 
 }  // namespace
 
@@ -94,15 +78,6 @@ int seedq_q4_gemv(const uint32_t* d_codes, const void* d_scale, const uint8_t* d
   return result(launch_q4_gemv(q, nvec, d_x, xtype, ldx, d_y, ytype, ldy, d_workspace,
                                static_cast<hipStream_t>(hip_stream)));
 }
-
-namespace {
-
-bool logits_ok(int64_t nrows, int64_t vocab, int64_t ld) {
-  return nrows >= 0 && nrows < (int64_t(1) << 31) && vocab >= 1 && vocab < (int64_t(1) << 31) &&
-         ld_ok(ld, vocab);
-}
-
-}  // namespace
 
 size_t seedq_token_logprobs_workspace_bytes(int64_t nrows, int64_t vocab, int32_t top) {
   if (nrows <= 0 || !logits_ok(nrows, vocab, vocab) || top < 0 || top > SEEDQ_MAX_TOP) return 0;

@@ -1,0 +1,204 @@
+"""The operators of seedq_mx4.h and seedq_beam.h without a GPU: exported symbols, argument
+errors (reported before anything touches a GPU), the helpers' refusals, and the oracle's own
+definitions against values worked out by hand."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from oracle import beam as obeam
+from oracle import mx4 as omx
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL, EUNSUPPORTED, EWORKSPACE = -1, -2, -6
+
+
+@pytest.fixture(scope="module")
+def sq():
+    import paper_2609_38477_amd as sq
+    if not os.path.exists(sq.LIB_PATH):
+        from paper_2609_38477_amd import build
+        build.build()
+    return sq
+
+
+@pytest.mark.parametrize("header,count", [("seedq_mx4.h", 7), ("seedq_beam.h", 3)])
+def test_every_declared_symbol_is_exported_and_wrapped(sq, header, count):
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", header)).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(seedq_[a-z0-9_]+)\s*\(", text)))
+    assert len(names) == count
+    raw = ctypes.CDLL(sq.LIB_PATH)
+    for n in names:
+        assert hasattr(raw, n) and hasattr(sq, n), n
+
+
+def test_quantize_and_dequantize_argument_errors(sq):
+    L = sq.mx4.lib()
+
+    def quantize(W=256, type=0, ldw=64, rows=4, cols=64, codes=256, scale=257):
+        return L.seedq_mx4_quantize(W, type, ldw, rows, cols, codes, scale, None)
+
+    def dequantize(codes=256, scale=257, rows=4, cols=64, W=256, type=0, ldw=64):
+        return L.seedq_mx4_dequantize(codes, scale, rows, cols, W, type, ldw, None)
+
+    for f in (quantize, dequantize):
+        for bad in (dict(W=None), dict(codes=None), dict(scale=None), dict(rows=0), dict(rows=-1),
+                    dict(cols=0), dict(cols=12), dict(ldw=63), dict(codes=264), dict(W=258),
+                    dict(type=1, W=257), dict(rows=1 << 31, cols=64), dict(ldw=1 << 41)):
+            assert f(**bad) == EINVAL, bad
+        for bad in (dict(type=3), dict(type=-1)):
+            assert f(**bad) == EUNSUPPORTED, bad
+    for c, words in ((8, 4), (32, 4), (40, 8), (4096, 512), (0, 0), (-8, 0), (12, 0)):
+        assert sq.seedq_mx4_row_words(c) == words
+
+
+def test_gemv_and_matmul_argument_errors(sq):
+    L = sq.mx4.lib()
+
+    def gemv(codes=256, scale=256, rows=4, cols=64, nvec=1, x=256, xt=2, ldx=64, y=256, yt=2, ldy=4,
+             ws=256, nws=1 << 30):
+        return L.seedq_mx4_gemv(codes, scale, rows, cols, nvec, x, xt, ldx, y, yt, ldy, ws, nws, None)
+
+    for bad in (dict(x=None), dict(y=None), dict(codes=None), dict(scale=None), dict(nvec=-1),
+                dict(cols=60), dict(rows=0), dict(ldx=63), dict(ldy=3), dict(x=257), dict(y=257),
+                dict(xt=0, yt=0, x=258), dict(yt=0, y=258), dict(codes=8), dict(nvec=1 << 25)):
+        assert gemv(**bad) == EINVAL, bad
+    for bad in (dict(xt=7), dict(yt=7), dict(xt=0, yt=1), dict(xt=1, yt=2)):
+        assert gemv(**bad) == EUNSUPPORTED, bad
+    assert gemv(nvec=0, x=None, y=None) == 0          # nothing to do
+
+    def matmul(ac=256, asc=256, na=4, bc=256, bs=256, nb=8, cols=64, y=256, yt=0, ldy=8, ws=256, nws=1 << 30):
+        return L.seedq_mx4_matmul(ac, asc, na, bc, bs, nb, cols, y, yt, ldy, ws, nws, None)
+
+    for bad in (dict(ac=None), dict(asc=None), dict(bc=None), dict(bs=None), dict(y=None), dict(na=-1),
+                dict(nb=0), dict(cols=60), dict(ldy=7), dict(y=258), dict(yt=1, y=257), dict(ac=264),
+                dict(bc=264), dict(na=1 << 31), dict(nb=1 << 31)):
+        assert matmul(**bad) == EINVAL, bad
+    assert matmul(yt=3) == EUNSUPPORTED
+    assert matmul(na=0, ac=None, asc=None, y=None) == 0
+    for f, need in ((lambda **k: gemv(rows=4096, cols=4096, ldx=4096, ldy=4096, **k),
+                     lambda n: sq.seedq_mx4_gemv_workspace_bytes(4096, 4096, n, 2)),
+                    (lambda nvec, **k: matmul(na=nvec, nb=4096, cols=4096, ldy=4096, **k),
+                     lambda n: sq.seedq_mx4_matmul_workspace_bytes(n, 4096, 4096))):
+        for n in (4, 64, 512):
+            if need(n):
+                for bad in (dict(ws=None), dict(nws=need(n) - 1), dict(ws=264)):
+                    assert f(nvec=n, **bad) == EWORKSPACE, (n, bad)
+    assert sq.seedq_mx4_gemv_workspace_bytes(0, 64, 1, 0) == 0
+    assert sq.seedq_mx4_matmul_workspace_bytes(0, 4, 64) == 0
+
+
+def test_select_argument_errors(sq):
+    L = sq.beam.lib()
+
+    def select(x=256, type=0, ld=100, batch=2, beams=4, vocab=100, scores=256, finished=None, pad=0, top=4,
+               score=256, parent=256, token=256, ws=256, nws=1 << 30):
+        return L.seedq_beam_select(x, type, ld, batch, beams, vocab, scores, finished, pad, top, score,
+                                   parent, token, ws, nws, None)
+
+    for bad in (dict(x=None), dict(scores=None), dict(score=None), dict(parent=None), dict(token=None),
+                dict(ld=99), dict(batch=-1), dict(beams=0), dict(beams=33), dict(vocab=0), dict(top=0),
+                dict(top=33), dict(x=258), dict(scores=258), dict(score=258), dict(parent=260),
+                dict(token=260), dict(finished=256, pad=-1), dict(batch=1 << 30), dict(vocab=1 << 31)):
+        assert select(**bad) == EINVAL, bad
+    assert select(type=4) == EUNSUPPORTED
+    for bad in (dict(ws=None), dict(ws=264), dict(nws=sq.seedq_beam_select_workspace_bytes(2, 4, 100, 4) - 1)):
+        assert select(**bad) == EWORKSPACE, bad
+    assert select(batch=0, x=None) == 0
+    for bad in ((0, 4, 100, 4), (2, 33, 100, 4), (2, 4, 0, 4), (2, 4, 100, 33)):
+        assert sq.seedq_beam_select_workspace_bytes(*bad) == 0
+
+
+def test_reorder_argument_errors(sq):
+    L = sq.beam.lib()
+
+    def reorder(parent=256, batch=2, inb=4, outb=4, n=1, **over):
+        f = dict(d_src=4096, d_dst=1 << 20, src_row=100, dst_row=100, src_outer=50, dst_outer=50, outer=2, inner=50)
+        f.update(over)
+        states = (sq.BeamState * 1)(sq.BeamState(**f))
+        return L.seedq_beam_reorder(states, n, parent, batch, inb, outb, None)
+
+    for bad in (dict(parent=None), dict(parent=260), dict(batch=-1), dict(inb=0), dict(outb=33), dict(inb=33),
+                dict(n=-1), dict(n=4097), dict(d_src=None), dict(d_dst=None), dict(outer=-1), dict(inner=-1),
+                dict(dst_row=99), dict(dst_outer=49), dict(src_row=-1), dict(src_outer=-1),
+                dict(d_dst=4096, src_row=101), dict(d_dst=4096, dst_outer=49, src_outer=50),
+                dict(d_dst=4096, inb=3), dict(inner=1 << 43), dict(outer=1 << 32),
+                dict(dst_row=50, dst_outer=399)):
+        assert reorder(**bad) == EINVAL, bad
+    assert reorder(batch=0, parent=None) == 0 and reorder(n=0, parent=None) == 0
+    assert L.seedq_beam_reorder(None, 1, 256, 2, 4, 4, None) == EINVAL
+
+
+def test_helpers_refuse_tensors_on_the_host(sq):
+    import torch
+    W = torch.zeros(4, 64)
+    with pytest.raises(ValueError):
+        sq.mx4_quantize(W)
+    with pytest.raises(TypeError):
+        sq.mx4_quantize(W.double())
+    with pytest.raises(ValueError):
+        sq.mx4_quantize(W[0])
+    q = sq.Mx4Weights(torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, 2, dtype=torch.uint8), 4, 64)
+    with pytest.raises(ValueError):
+        sq.mx4_dequantize(q)
+    with pytest.raises(ValueError):
+        sq.mx4_gemv(q, W)
+    with pytest.raises(ValueError):
+        sq.mx4_gemv(q, torch.zeros(4, 63))
+    with pytest.raises(TypeError):
+        sq.mx4_gemv(q, W, torch.float16)
+    with pytest.raises(ValueError):
+        sq.mx4_matmul(q, q)
+    with pytest.raises(TypeError):
+        sq.mx4_matmul(q, q, torch.float64)
+    x, scores = torch.zeros(4, 9), torch.zeros(2, 2)
+    for bad in (lambda: sq.beam_select(x, scores, 2), lambda: sq.beam_select(x, scores[0], 2),
+                lambda: sq.beam_reorder(x, torch.zeros(2, 2, dtype=torch.int64)),
+                lambda: sq.beam_reorder(x, torch.zeros(2, dtype=torch.int64)),
+                lambda: sq.beam_reorder(x, torch.zeros(2, 33, dtype=torch.int64))):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_pieces_of_rows(sq):
+    import torch
+    from paper_2609_38477_amd.beam import _pieces, _split
+    t = torch.zeros(4, 3, 10, 8)
+    assert _pieces(t) == (960, 1, 0, 960)
+    assert _pieces(t[:, :, :7]) == (960, 3, 320, 224)
+    assert _pieces(t[:, :, 2:7, :5]) is None
+    assert _pieces(t[:, 1, :, 3]) == (960, 10, 32, 4)
+    assert _pieces(t[:, 1:2, 3, :]) == (960, 1, 0, 32)
+    assert _pieces(t.transpose(1, 2)) is None
+    assert _pieces(torch.zeros(5, dtype=torch.int64)) == (8, 1, 0, 8)
+    a, b = _split(_pieces(t[:, :, :7]), (672, 1, 0, 672))
+    assert a == (960, 3, 320, 224) and b == (672, 3, 224, 224)
+    assert _split((64, 2, 32, 12), (64, 3, 20, 8)) == (None, None)
+
+
+# ---------------------------------------------------------------- the oracle's definitions
+
+def test_oracle_quantiser_by_hand():
+    w = np.zeros((1, 40))
+    w[0, :9] = [6.0, 0.25, 0.75, -0.2, -5.0, 2.5, 3.5, 7.99, -0.0]
+    w[0, 32:35] = [0.3, 0.11, -0.05]
+    codes, scale = omx.quantize(w)
+    assert scale.tolist() == [[127, 123]]              # 7.99 = 2^2 .., 0.3 = 2^-2 ..
+    assert codes[0, :9].tolist() == [7, 0, 2, 8, 14, 4, 6, 7, 8]
+    assert codes[0, 32:35].tolist() == [6, 4, 10]      # 4.8, 1.76 and -0.8 sixteenths
+    assert omx.values(codes, scale)[0, 32:35].tolist() == [0.25, 0.125, -0.0625]
+    w[0, 3] = np.nan
+    assert omx.quantize(w)[1].tolist() == [[255, 123]]
+
+
+def test_oracle_selection_and_reordering_by_hand():
+    x = np.log(np.array([[1.0, 2.0, 1.0], [1.0, 1.0, 2.0]]))
+    got = obeam.select(x, [0.0, np.log(0.5)], None, 0, 4)
+    assert [g[1:] for g in got] == [(0, 1), (0, 0), (0, 2), (1, 2)]
+    assert np.allclose([g[0] for g in got], np.log([0.5, 0.25, 0.25, 0.25]))
+    got = obeam.select(x, [-9.0, -1.0], [False, True], 7, 5)
+    assert got[0] == (-1.0, 1, 7) and got[4] == (-np.inf, -1, -1)
+    state = np.arange(4).reshape(4, 1)
+    assert obeam.reorder(state, np.array([[1, 1, -1], [0, 5, 1]])).ravel().tolist() == [1, 1, 0, 2, 0, 3]
