@@ -1,7 +1,9 @@
 // Products of two matrices of microscaled 4-bit floats on the matrix core, which takes the
 // codes and the blocks' exponents as they lie in memory: lane l of a 32x32x64 product holds
-// the 16 bytes of block l / 32 of row l % 32 and that block's exponent.
+// the 16 bytes of block l / 32 of row l % 32 and that block's exponent, of a 16x16x128
+// product those of block l / 16 of row l % 16.
 #include <algorithm>
+#include <type_traits>
 
 #include "seedq_mx4_internal.h"
 #include "seedq_ops_device.h"
@@ -10,60 +12,340 @@ namespace seedq {
 namespace {
 
 typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t uint32x2 __attribute__((ext_vector_type(2)));
+// Bytes anywhere.
+typedef uint32x2 uint32x2_byte __attribute__((aligned(1)));
+typedef uint32x4 uint32x4_byte __attribute__((aligned(1)));
 
 __device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v) {
   if (ytype == SEEDQ_F32) static_cast<float*>(y)[at] = v;
   else static_cast<uint16_t*>(y)[at] = ytype == SEEDQ_F16 ? F16::narrow(v) : BF16::narrow(v);
 }
 
+constexpr int kFp4 = 4;   // the instructions' number for the type
 __device__ __forceinline__ intx8 fp4_operand(uint32x4 c) {
   return intx8{int(c[0]), int(c[1]), int(c[2]), int(c[3]), 0, 0, 0, 0};
 }
 
-// A wave makes 32 x 32 of Y.
-__global__ void __launch_bounds__(256)
-matmul_kernel(Mx4 a, Mx4 b, void* __restrict__ y, int ytype, int64_t ldy) {
-  const int lane = int(threadIdx.x & 63), n = lane & 31, kg = lane >> 5;
-  const int64_t j0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * 32, j = std::min(j0 + n, b.nrows - 1);
-  if (j0 >= b.nrows) return;
-  for (int64_t i0 = int64_t(blockIdx.y) * 32; i0 < a.nrows; i0 += int64_t(gridDim.y) * 32) {
-    const int64_t i = std::min(i0 + n, a.nrows - 1);
-    floatx16 acc = {};
-    for (int64_t k = kg; k < b.nblocks + kg; k += 2) {
-      uint32x4 ca = {0u, 0u, 0u, 0u}, cb = {0u, 0u, 0u, 0u};
-      int sa = 0, sb = 0;
-      if (k < b.nblocks) {
-        ca = *reinterpret_cast<const uint32x4*>(a.codes + i * a.row_words + k * 4);
-        cb = *reinterpret_cast<const uint32x4*>(b.codes + j * b.row_words + k * 4);
-        sa = a.scale[i * a.nblocks + k];
-        sb = b.scale[j * b.nblocks + k];
-      }
-      acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(ca), fp4_operand(cb), acc, 4, 4, 0,
-                                                            sa, 0, sb);
-    }
+// ---------------------------------------------------------------- few rows of A
+
+// 16 AT rows of A against 16 rows of B a workgroup. The waves divide the columns in steps of
+// 512, whose codes and exponents a lane reads straight into registers, the next step's
+// during the products; their sums meet in LDS in order. A's rows are the same for all
+// workgroups and come from the caches.
+constexpr int kStep = 4;        // products of a step
+constexpr int kFewWaves = 8;
+
+template <int AT>
+__global__ void __launch_bounds__(64 * kFewWaves)
+few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ldy, float* __restrict__ partial) {
+  __shared__ float part[kFewWaves][AT * 4 * 64];
+  const int lane = int(threadIdx.x & 63), n = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), waves = int(blockDim.x >> 6);
+  const int64_t j0 = int64_t(blockIdx.x) * 16;
+  const int64_t steps = (b.nblocks + 4 * kStep - 1) / (4 * kStep);
+  const int64_t shares = int64_t(splits) * waves, mine = int64_t(blockIdx.y) * waves + wave;
+  const int64_t from = steps * mine / shares, to = steps * (mine + 1) / shares;
+  struct Side {
+    const uint32_t* codes;
+    const uint8_t* scale;
+  };
+  struct Piece {
+    uint32x4 code[kStep], s;
+  };
+  const int64_t nblocks = b.nblocks;
+  const auto row_of = [&](const Mx4& m, int64_t r) __attribute__((always_inline)) {
+    r = std::min(r, m.nrows - 1);
+    return Side{m.codes + r * m.row_words, m.scale + r * m.nblocks};
+  };
+  // Past the last block: its codes again under exponent 0 on both sides, which is 2^-254.
+  const auto load = [&](const Side& side, Piece& k, int64_t step) __attribute__((always_inline)) {
+    const int64_t b0 = step * (4 * kStep);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t row = i0 + 8 * (e >> 2) + 4 * kg + (e & 3);
-      if (row < a.nrows && j0 + n < b.nrows) store_y(y, ytype, row * ldy + j0 + n, acc[e]);
+    for (int d = 0; d < kStep; ++d)
+      k.code[d] = *reinterpret_cast<const uint32x4*>(side.codes + std::min(b0 + 4 * d + kg, nblocks - 1) * 4);
+    if (b0 + 4 * kStep <= nblocks) {
+      k.s = *reinterpret_cast<const uint32x4_byte*>(side.scale + b0);
+    } else {
+#pragma unroll
+      for (int d = 0; d < kStep; ++d) {
+        const int64_t block = b0 + 4 * d + kg;
+        k.s[d] = block < nblocks ? uint32_t(side.scale[block]) << (8 * kg) : 0u;
+      }
     }
+  };
+  Side arow[AT];
+#pragma unroll
+  for (int t = 0; t < AT; ++t) arow[t] = row_of(a, 16 * t + n);
+  const Side brow = row_of(b, j0 + n);
+  floatx4 acc[AT] = {};
+  Piece ka[2][AT], kb[2];
+  const auto fetch = [&](int buf, int64_t step) __attribute__((always_inline)) {
+    load(brow, kb[buf], step);
+#pragma unroll
+    for (int t = 0; t < AT; ++t) load(arow[t], ka[buf][t], step);
+  };
+  const auto use = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int d = 0; d < kStep; ++d) {
+      const int sb = int(kb[buf].s[d] >> (8 * kg));
+#pragma unroll
+      for (int t = 0; t < AT; ++t)
+        acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            fp4_operand(ka[buf][t].code[d]), fp4_operand(kb[buf].code[d]), acc[t], kFp4, kFp4, 0,
+            int(ka[buf][t].s[d] >> (8 * kg)), 0, sb);
+    }
+  };
+  if (from < to) fetch(0, from);
+  for (int64_t s = from; s < to; s += 2) {
+    if (s + 1 < to) fetch(1, s + 1);
+    use(0);
+    if (s + 1 >= to) break;
+    if (s + 2 < to) fetch(0, s + 2);
+    use(1);
   }
+#pragma unroll
+  for (int t = 0; t < AT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][(t * 4 + i) * 64 + lane] = acc[t][i];
+  __syncthreads();
+  // row 4 kg + i of A and row n of B lie in lane 16 kg + n, register i
+  for (int k = int(threadIdx.x); k < AT * 256; k += int(blockDim.x)) {
+    float total = part[0][k];
+    for (int w = 1; w < waves; ++w) total += part[w][k];
+    const int64_t v = (k >> 8) * 16 + ((k & 63) >> 4) * 4 + ((k >> 6) & 3), r = j0 + (k & 15);
+    if (v >= a.nrows || r >= b.nrows) continue;
+    if (splits > 1) partial[(int64_t(blockIdx.y) * a.nrows + v) * b.nrows + r] = total;
+    else store_y(y, ytype, v * ldy + r, total);
+  }
+}
+
+// ---------------------------------------------------------------- tiles
+
+// A workgroup of WM x WN waves makes 32 MT WM rows of A x 32 NT WN rows of B, a wave
+// 32 MT x 32 NT, in stages of 256 columns: eight blocks, 128 bytes a row, that go to LDS
+// without passing registers, the next stage's during the products. Block j of row r lies at
+// place j ^ (r / 2 % 8) of the row's eight, so that the 16 bytes that neighbouring lanes
+// read, of neighbouring rows, spread over all banks. A lane's four exponents of a stage are
+// one register that the products pick their byte of.
+constexpr int kBlocks = 8;   // of a stage
+
+__device__ __forceinline__ void to_lds16(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from),
+                                   (__attribute__((address_space(3))) void*)(to), 16, 0, 0);
+}
+
+template <int MT, int NT, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2)
+tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict__ y, int ytype,
+            int64_t ldy, float* __restrict__ partial) {
+  constexpr int kWaves = WM * WN, kRowsA = 32 * MT * WM, kRowsB = 32 * NT * WN;
+  constexpr int kLoads = (kRowsA + kRowsB) / 8 / kWaves;   // of 8 rows a wave
+  static_assert((kRowsA + kRowsB) % (8 * kWaves) == 0 && kRowsA % 8 == 0, "whole loads");
+  extern __shared__ uint32x4 lds[];   // [2][kRowsA + kRowsB][8]
+  // Workgroups go to the eight XCDs in turn: those of one XCD that run together share
+  // rows of B in its L2.
+  const unsigned id = blockIdx.x, xcd = id & 7, j8 = id >> 3;
+  const int at = int(j8 % unsigned(a_tiles));
+  const int unit = int(j8 / unsigned(a_tiles)) * 8 + int(xcd);
+  if (unit >= b_tiles * splits) return;
+  const int bt = unit % b_tiles, split = unit / b_tiles;
+  const int64_t nblocks = b.nblocks, stages = (nblocks + kBlocks - 1) / kBlocks;
+  const int64_t s0 = stages * split / splits, s1 = stages * (split + 1) / splits;
+  const int lane = int(threadIdx.x & 63), n = lane & 31, kg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
+  const int wm = wave % WM, wn = wave / WM;
+  const int64_t i0 = int64_t(at) * kRowsA, j0 = int64_t(bt) * kRowsB;
+  // this lane's rows and blocks of the loads
+  const uint32_t* from[kLoads];
+  int block[kLoads];
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const int r = (k * kWaves + wave) * 8 + (lane >> 3);
+    block[k] = (lane & 7) ^ ((r >> 1) & 7);
+    from[k] = r < kRowsA ? a.codes + std::min(i0 + r, a.nrows - 1) * a.row_words
+                         : b.codes + std::min(j0 + r - kRowsA, b.nrows - 1) * b.row_words;
+  }
+  const uint8_t* sfrom[MT + NT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+    sfrom[t] = a.scale + std::min(i0 + (wm * MT + t) * 32 + n, a.nrows - 1) * nblocks;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    sfrom[MT + t] = b.scale + std::min(j0 + (wn * NT + t) * 32 + n, b.nrows - 1) * nblocks;
+  struct Scales {
+    uint32x2 s[MT + NT];
+  };
+  // Past the last block: its codes again under exponent 0 on both sides, which is 2^-254.
+  const auto fetch = [&](int64_t stage, int buf, Scales& k) __attribute__((always_inline)) {
+    const int64_t b0 = stage * kBlocks;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      to_lds16(from[i] + std::min(b0 + block[i], nblocks - 1) * 4,
+               &lds[(buf * (kRowsA + kRowsB) + (i * kWaves + wave) * 8) * 8]);
+    if (b0 + kBlocks <= nblocks) {
+#pragma unroll
+      for (int t = 0; t < MT + NT; ++t) k.s[t] = *reinterpret_cast<const uint32x2_byte*>(sfrom[t] + b0);
+    } else {
+#pragma unroll
+      for (int t = 0; t < MT + NT; ++t) {
+        k.s[t] = uint32x2{0u, 0u};
+        for (int j = 0; j < kBlocks && b0 + j < nblocks; ++j)
+          k.s[t][j >> 2] |= uint32_t(sfrom[t][b0 + j]) << (8 * (j & 3));
+      }
+    }
+  };
+  floatx16 acc[MT][NT] = {};
+  Scales cur;
+  fetch(s0, 0, cur);
+  const uint32_t pick = kg ? 0x07050301u : 0x06040200u;   // blocks kg, 2 + kg, 4 + kg, 6 + kg
+  const int swizzle = (n >> 1) & 7;
+  for (int64_t s = s0; s < s1; ++s) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this stage's codes are in LDS
+    __syncthreads();                                   // everybody's; the other buffer is free
+    const int buf = int(s - s0) & 1;
+    Scales next = cur;
+    if (s + 1 < s1) fetch(s + 1, buf ^ 1, next);
+    int sc[MT + NT];
+#pragma unroll
+    for (int t = 0; t < MT + NT; ++t) sc[t] = int(__builtin_amdgcn_perm(cur.s[t][1], cur.s[t][0], pick));
+    const uint32x4* la = lds + (buf * (kRowsA + kRowsB) + wm * MT * 32 + n) * 8;
+    const uint32x4* lb = lds + (buf * (kRowsA + kRowsB) + kRowsA + wn * NT * 32 + n) * 8;
+    const auto products = [&](auto kk) __attribute__((always_inline)) {
+      constexpr int K = decltype(kk)::value;
+      intx8 ca[MT], cb[NT];
+      const int place = (2 * K + kg) ^ swizzle;
+#pragma unroll
+      for (int t = 0; t < MT; ++t) ca[t] = fp4_operand(la[t * 256 + place]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) cb[t] = fp4_operand(lb[t * 256 + place]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ca[i], cb[j], acc[i][j], kFp4, kFp4,
+                                                                      K, sc[i], K, sc[MT + j]);
+    };
+    products(std::integral_constant<int, 0>{});
+    products(std::integral_constant<int, 1>{});
+    products(std::integral_constant<int, 2>{});
+    products(std::integral_constant<int, 3>{});
+    cur = next;
+  }
+  // register e of lane l: row 8 (e / 4) + 4 (l / 32) + e % 4 of A, row l % 32 of B
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int64_t r = j0 + (wn * NT + j) * 32 + n;
+    if (r >= b.nrows) continue;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int64_t v = i0 + (wm * MT + i) * 32 + 8 * (e >> 2) + 4 * kg + (e & 3);
+        if (v >= a.nrows) continue;
+        if (splits > 1) partial[(split * a.nrows + v) * b.nrows + r] = acc[i][j][e];
+        else store_y(y, ytype, v * ldy + r, acc[i][j][e]);
+      }
+  }
+}
+
+// The splits of the columns added in order.
+__global__ void __launch_bounds__(256)
+join_kernel(const float* __restrict__ partial, int splits, int64_t na, int64_t nb, void* __restrict__ y,
+            int ytype, int64_t ldy) {
+  const int64_t v = blockIdx.y;
+  const int64_t r = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (r >= nb) return;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) sum += partial[(s * na + v) * nb + r];
+  store_y(y, ytype, v * ldy + r, sum);
+}
+
+// Rows of A of one pass: the grids stay small, and so does the workspace.
+constexpr int64_t kMaxVecs = 32768;
+constexpr int kFewRows = 64;
+
+struct Plan {
+  int tile;   // rows of a tile, 0 for the kernel of few rows
+  int a_tiles, b_tiles, splits, waves;
+  size_t partial;
+};
+Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
+  Plan p{};
+  if (na <= kFewRows) {
+    const int64_t steps = (nblocks + 4 * kStep - 1) / (4 * kStep);
+    p.b_tiles = int((nb + 15) / 16);
+    p.waves = int(std::min<int64_t>(kFewWaves, steps));
+    p.splits = int(std::max<int64_t>(1, std::min<int64_t>({256 / p.b_tiles, steps / (2 * p.waves), 16})));
+  } else {
+    const int64_t stages = (nblocks + kBlocks - 1) / kBlocks;
+    const auto tiles = [&](int64_t t) { return ((na + t - 1) / t) * ((nb + t - 1) / t); };
+    p.tile = na > 128 && tiles(256) >= 256 ? 256 : 128;
+    p.a_tiles = int((na + p.tile - 1) / p.tile), p.b_tiles = int((nb + p.tile - 1) / p.tile);
+    p.splits = int(std::max<int64_t>(
+        1, std::min<int64_t>({512 / (int64_t(p.a_tiles) * p.b_tiles), stages / 4, 16})));
+  }
+  p.partial = p.splits > 1 ? align256(size_t(p.splits) * na * nb * sizeof(float)) : 0;
+  return p;
+}
+
+// Bytes for up to kMaxRows rows of B.
+size_t rows_bytes(int64_t na, int64_t nb, int64_t nblocks) {
+  size_t need = plan(std::min(na, kMaxVecs), nb, nblocks).partial;
+  if (na > kMaxVecs && na % kMaxVecs) need = std::max(need, plan(na % kMaxVecs, nb, nblocks).partial);
+  return need;
+}
+
+hipError_t launch(const Mx4& a, const Mx4& b, void* d_y, int ytype, int64_t ldy, float* partial,
+                  hipStream_t stream) {
+  const Plan p = plan(a.nrows, b.nrows, b.nblocks);
+  if (p.tile == 0) {
+    auto go = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3(unsigned(p.b_tiles), unsigned(p.splits)), dim3(64 * p.waves), 0, stream,
+                         a, b, p.splits, d_y, ytype, ldy, partial);
+    };
+    if (a.nrows <= 16) go(few_kernel<1>);
+    else if (a.nrows <= 32) go(few_kernel<2>);
+    else go(few_kernel<4>);
+  } else {
+    const int64_t units = (int64_t(p.b_tiles) * p.splits + 7) / 8 * 8;
+    auto go = [&](auto kern, int waves) {
+      hipLaunchKernelGGL(kern, dim3(unsigned(units * p.a_tiles)), dim3(64 * waves), size_t(4) * p.tile * 128,
+                         stream, a, b, p.a_tiles, p.b_tiles, p.splits, d_y, ytype, ldy, partial);
+    };
+    if (p.tile == 256) go(tile_kernel<4, 2, 2, 4>, 8);
+    else go(tile_kernel<2, 2, 2, 2>, 4);
+  }
+  if (p.splits > 1)
+    hipLaunchKernelGGL(join_kernel, dim3(unsigned((b.nrows + 255) / 256), unsigned(a.nrows)), dim3(256), 0,
+                       stream, partial, p.splits, a.nrows, b.nrows, d_y, ytype, ldy);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t mx4_matmul_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t mx4_matmul_workspace_bytes(int64_t na, int64_t nb, int64_t ncols) {
+  const int64_t nblocks = (ncols + kMxBlock - 1) / kMxBlock;
+  size_t need = rows_bytes(na, std::min(nb, kMaxRows), nblocks);
+  if (nb > kMaxRows && nb % kMaxRows) need = std::max(need, rows_bytes(na, nb % kMaxRows, nblocks));
+  return need;
+}
 
-hipError_t launch_mx4_matmul(const Mx4& a, const Mx4& all, void* d_y, int ytype, int64_t ldy, void*,
+hipError_t launch_mx4_matmul(const Mx4& a, const Mx4& b, void* d_y, int ytype, int64_t ldy, void* d_ws,
                              hipStream_t stream) {
-  for (int64_t r = 0; r < all.nrows; r += kMaxRows) {
-    const Mx4 b = all.rows(r);
-    hipLaunchKernelGGL(matmul_kernel,
-                       dim3(unsigned((b.nrows + 127) / 128), unsigned(std::min<int64_t>((a.nrows + 31) / 32, 4096))),
-                       dim3(256), 0, stream, a, b, static_cast<char*>(d_y) + r * (ytype == SEEDQ_F32 ? 4 : 2),
-                       ytype, ldy);
-  }
-  return hipGetLastError();
+  const int64_t size = ytype == SEEDQ_F32 ? 4 : 2;
+  for (int64_t r = 0; r < b.nrows; r += kMaxRows)
+    for (int64_t v = 0; v < a.nrows; v += kMaxVecs) {
+      Mx4 rows = a.rows(v);
+      rows.nrows = std::min(kMaxVecs, a.nrows - v);
+      const hipError_t e = launch(rows, b.rows(r), static_cast<char*>(d_y) + (r + v * ldy) * size, ytype, ldy,
+                                  static_cast<float*>(d_ws), stream);
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
 }
 
 }  // namespace seedq
