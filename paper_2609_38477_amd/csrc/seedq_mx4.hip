@@ -7,7 +7,7 @@
 // conversion instructions take a power of two by its exponent field alone, 0 standing for
 // 2^-127, round to nearest even and saturate, which is the definition's rounding.
 #include "seedq_mx4_internal.h"
-#include "seedq_ops_device.h"
+#include "seedq_mx4_device.h"
 
 namespace seedq {
 namespace {
@@ -16,9 +16,6 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-
-// 2^(e - 127) as the conversions take it.
-__device__ __forceinline__ float mx_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
 
 // A wave: 64 words of one row.
 template <class T>

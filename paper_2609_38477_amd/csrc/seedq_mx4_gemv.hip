@@ -11,7 +11,7 @@
 #include <type_traits>
 
 #include "seedq_mx4_internal.h"
-#include "seedq_ops_device.h"
+#include "seedq_mx4_device.h"
 
 namespace seedq {
 namespace {
@@ -24,8 +24,13 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// 2^(e - 127) as the conversions take it.
-__device__ __forceinline__ float mx_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
+// Two of the weights of a word; which is a constant where this is inlined.
+__device__ __forceinline__ bf16x2 pair_of(uint32_t w, float scale, int which) {
+  return which == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+         : which == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+         : which == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                      : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+}
 
 // The eight weights of a word.
 __device__ __forceinline__ bf16x8 decode(uint32_t w, float scale) {
@@ -35,14 +40,6 @@ __device__ __forceinline__ bf16x8 decode(uint32_t w, float scale) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-
-__device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v) {
-  if (ytype == SEEDQ_F32) static_cast<float*>(y)[at] = v;
-  else static_cast<uint16_t*>(y)[at] = ytype == SEEDQ_F16 ? F16::narrow(v) : BF16::narrow(v);
-}
-
-// 16 bytes anywhere.
-typedef uint32x4 uint32x4_byte __attribute__((aligned(1)));
 
 // Pieces of a type, and the rows of a product that a vector takes up.
 template <class X>
@@ -323,7 +320,7 @@ batch_kernel(Mx4 q, int nvec, const typename X::raw* __restrict__ x, int64_t ldx
     }
   };
   const auto load = [&](Codes& k, int c) __attribute__((always_inline)) {
-    const int64_t b0 = int64_t(c0 + c) * 4;
+    const int64_t b0 = int64_t(c0 + c) * 4;   // q.nblocks >= 16
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) {
       // past the last block the last one again, of the same row: its x is zero
@@ -332,16 +329,8 @@ batch_kernel(Mx4 q, int nvec, const typename X::raw* __restrict__ x, int64_t ldx
       for (int t = 0; t < RT; ++t) k.code[d][t] = *reinterpret_cast<const uint32x4*>(crow[t] + block * 4);
     }
     // the exponents of the step's 16 blocks, the same for the four lanes of a row
-    if (b0 + 16 <= q.nblocks) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) k.s[t] = *reinterpret_cast<const uint32x4_byte*>(srow[t] + b0);
-    } else {
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int d = 0; d < kDeep; ++d)
-          k.s[t][d] = uint32_t(srow[t][std::min(b0 + 4 * d + kg, q.nblocks - 1)]) << (8 * kg);
-    }
+    for (int t = 0; t < RT; ++t) k.s[t] = *reinterpret_cast<const uint32x4_byte*>(srow[t] + std::min(b0, q.nblocks - 16));
   };
   Codes k0, k1;   // the first step's are on their way while x is laid out
   int64_t b = int64_t(blockIdx.x) * cut.groups;
@@ -363,13 +352,16 @@ batch_kernel(Mx4 q, int nvec, const typename X::raw* __restrict__ x, int64_t ldx
     const bool some = b + group < tiles;
     floatx4 acc[XT][RT] = {};
     const auto use = [&](const Codes& k, int c) __attribute__((always_inline)) {
+      uint32x4 se[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) se[t] = after_bytes(k.s[t], int64_t(c0 + c) * 4 + 16 - q.nblocks);
 #pragma unroll
       for (int d = 0; d < kDeep; ++d) {
         if (c + d >= to) break;
         const uint32x4* xs = lds + (c + d) * 16 * rows_x;
         float s[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) s[t] = mx_scale(__builtin_amdgcn_ubfe(k.s[t][d], 8 * kg, 8));
+        for (int t = 0; t < RT; ++t) s[t] = mx_scale(__builtin_amdgcn_ubfe(se[t][d], 8 * kg, 8));
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           bf16x8 a[XT];
@@ -475,7 +467,8 @@ join_kernel(const float* __restrict__ partial, int panels, int64_t nvec, int64_t
 constexpr int kFrags = 4;       // of 64 lanes x 16 bytes: a chunk of 64 columns, 32 vectors, each piece
 constexpr int kTileVecs = 32;
 
-// A workgroup: 32 vectors, four chunks at a time. Fragments [vector tile][chunk][piece][4][lane].
+// A workgroup: 32 vectors, four chunks at a time. Fragments
+// [vector tile][chunk][piece, the smallest first][4][lane].
 template <class X>
 __global__ void __launch_bounds__(256)
 frag_kernel(const typename X::raw* __restrict__ x, int64_t ldx, int64_t nvec, int64_t ncols,
@@ -495,15 +488,9 @@ frag_kernel(const typename X::raw* __restrict__ x, int64_t ldx, int64_t nvec, in
       if (v < nvec && c < ncols) split8<X>(x + v * ldx + c, piece);
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        frag[(((tile * chunks + chunk) * P + p) * kFrags + (k & 3)) * 64 + (k >> 2) * 32 + m] = piece[p];
+        frag[(((tile * chunks + chunk) * P + (P - 1 - p)) * kFrags + (k & 3)) * 64 + (k >> 2) * 32 + m] = piece[p];
     }
   }
-}
-
-// 16 bytes a lane to LDS, lane after lane.
-__device__ __forceinline__ void to_lds16(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from),
-                                   (__attribute__((address_space(3))) void*)(to), 16, 0, 0);
 }
 
 template <int P, int MT, int RT, int C>
@@ -520,7 +507,7 @@ gemm_kernel(Mx4 q, int64_t nvec, const uint32x4* __restrict__ frags, int64_t chu
   const int unit = int(j8 / unsigned(vec_tiles)) * 8 + int(xcd);
   if (unit >= row_tiles * splits) return;
   const int rt = unit % row_tiles, split = unit / row_tiles;
-  const int64_t stages = (chunks + C - 1) / C;
+  const int64_t stages = chunks / C;
   const int64_t s0 = stages * split / splits, s1 = stages * (split + 1) / splits;
   const int lane = int(threadIdx.x & 63);
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
@@ -538,73 +525,102 @@ gemm_kernel(Mx4 q, int64_t nvec, const uint32x4* __restrict__ frags, int64_t chu
     uint32x4 code[RT][C];
     uint8_t s[RT][C];   // as they lie in memory: nothing waits for them at once
   };
-  const auto fetch = [&](int64_t stage, int buf, Rows& k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < C * MT * kEach / 4; ++i) {
+  // The loads of a stage one by one: fragments, codes, exponents.
+  constexpr int kDma = C * MT * kEach / 4, kLoads = kDma + 2 * RT * C;
+  const auto fetch = [&](int64_t stage, int buf, Rows& k, int i) __attribute__((always_inline)) {
+    if (i < kDma) {
       const int f = 4 * i + wave;   // [chunk][tile][piece][4]
       const int c = f / (MT * kEach), m = f / kEach % MT, rest = f % kEach;
-      const int64_t chunk = std::min(stage * C + c, chunks - 1);
+      const int64_t chunk = stage * C + c;
       to_lds16(frags + ((int64_t(vt * MT + m) * chunks + chunk) * kEach + rest) * 64 + lane, &lds[buf][f * 64]);
+      return;
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      // past the last block the last one again, of the same row: its x is zero
-      const int64_t block = std::min((stage * C + c) * 2 + kg, q.nblocks - 1);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        k.code[t][c] = *reinterpret_cast<const uint32x4*>(crow[t] + block * 4);
-        k.s[t][c] = srow[t][block];
-      }
-    }
+    const int t = (i - kDma) % RT, c = (i - kDma) / RT % C;
+    // past the last block the last one again, of the same row: its x is zero
+    const int64_t block = std::min((stage * C + c) * 2 + kg, q.nblocks - 1);
+    if (i < kDma + RT * C) k.code[t][c] = *reinterpret_cast<const uint32x4*>(crow[t] + block * 4);
+    else k.s[t][c] = srow[t][block];
   };
   floatx16 acc[RT][MT] = {};
   Rows cur;
-  fetch(s0, 0, cur);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) fetch(s0, 0, cur, i);
   for (int64_t s = s0; s < s1; ++s) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this stage's fragments are in LDS
     __syncthreads();                                   // for everybody; the other buffer is free
     const int buf = int(s - s0) & 1;
-    Rows next = cur;
-    if (s + 1 < s1) fetch(s + 1, buf ^ 1, next);
+    Rows next;
+    const int64_t later = std::min(s + 1, s1 - 1);   // always, so that there is no branch
+    // Step (c, k) is 16 columns of each half of a chunk. Its fragments and weights are made
+    // ready between the products of the step before, in the order in which they are needed:
+    // left to itself the compiler reads a fragment right before its use. The next stage's
+    // loads are issued one by one between the first products.
+    bf16x8 a[2][MT * P];
+    bf16x2 w[2][RT][4];
+    float scale[RT][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (C > 1 && s * C + c >= chunks) break;
-      float scale[RT];
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) scale[t] = mx_scale(cur.s[t][c]);
+      for (int c = 0; c < C; ++c) scale[t][c] = mx_scale(cur.s[t][c]);
+    const auto fragment = [&](int i, int m) __attribute__((always_inline)) {
+      a[i & 1][m] = __builtin_bit_cast(
+          bf16x8, lds[buf][(((i / 4) * MT * P + m) * kFrags + i % 4) * 64 + lane]);
+    };
+    const auto convert = [&](int i, int j) __attribute__((always_inline)) {
+      const int t = j / 4;
+      w[i & 1][t][j % 4] = pair_of(cur.code[t][i / 4][i % 4], scale[t][i / 4], j % 4);
+    };
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        bf16x8 w[RT];
+    for (int m = 0; m < MT * P; ++m) fragment(0, m);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) w[t] = decode(cur.code[t][c][k], scale[t]);
+    for (int j = 0; j < 4 * RT; ++j) convert(0, j);
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+    for (int i = 0; i < 4 * C; ++i)
 #pragma unroll
-          for (int p = P - 1; p >= 0; --p) {   // the smallest pieces first
-            const bf16x8 a = __builtin_bit_cast(bf16x8, lds[buf][(((c * MT + m) * P + p) * kFrags + k) * 64 + lane]);
+      for (int m = 0; m < MT * P; ++m) {
+        constexpr int kGroups = 4 * C * MT * P;
+        for (int l = (i * MT * P + m) * 2 * kLoads / kGroups; l < (i * MT * P + m + 1) * 2 * kLoads / kGroups; ++l)
+          if (l < kLoads) fetch(later, buf ^ 1, next, l);
+        if (i + 1 < 4 * C) {
+          fragment(i + 1, m);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-              acc[t][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[t], acc[t][m], 0, 0, 0);
-          }
+          for (int j = 4 * RT * m / (MT * P); j < 4 * RT * (m + 1) / (MT * P); ++j) convert(i + 1, j);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const bf16x2* u = w[i & 1][t];
+          acc[t][m / P] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              a[i & 1][m], bf16x8{u[0][0], u[0][1], u[1][0], u[1][1], u[2][0], u[2][1], u[3][0], u[3][1]},
+              acc[t][m / P], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
     cur = next;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way to LDS when it is given up
   // register i of lane l: vector 8 (i / 4) + 4 (l / 32) + i % 4, row l % 32
+  const auto write = [&](auto type, void* to, int64_t ld) __attribute__((always_inline)) {
+    using Y = decltype(type);
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int64_t r = r0 + 32 * t + n;
-    if (r >= q.nrows) continue;
+    for (int t = 0; t < RT; ++t) {
+      const int64_t r = r0 + 32 * t + n;
+      if (r >= q.nrows) continue;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < MT; ++m) {
+        const int64_t v0 = int64_t(vt * MT + m) * kTileVecs + 4 * kg;
+        typename Y::raw* p = static_cast<typename Y::raw*>(to) + v0 * ld + r;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int64_t v = int64_t(vt * MT + m) * kTileVecs + 8 * (i >> 2) + 4 * kg + (i & 3);
-        if (v >= nvec) continue;
-        if (splits > 1) partial[(split * nvec + v) * q.nrows + r] = acc[t][m][i];
-        else store_y(y, ytype, v * ldy + r, acc[t][m][i]);
+        for (int i = 0; i < 16; ++i) {
+          const int v = 8 * (i >> 2) + (i & 3);
+          if (v0 + v < nvec) p[v * ld] = Y::narrow(acc[t][m][i]);
+        }
       }
-  }
+    }
+  };
+  if (splits > 1) write(F32{}, partial + split * nvec * q.nrows, q.nrows);
+  else if (ytype == SEEDQ_F32) write(F32{}, y, ldy);
+  else if (ytype == SEEDQ_F16) write(F16{}, y, ldy);
+  else write(BF16{}, y, ldy);
 }
 
 constexpr int kPanelBytes = 96 << 10;
@@ -683,7 +699,7 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   p.vec_tiles = int((tiles + p.mt - 1) / p.mt);
   p.rt = (nrows + 255) / 256 * p.vec_tiles >= 400 ? 2 : 1;
   p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
-  p.chunks = (ncols + 63) / 64;
+  p.chunks = (ncols + 127) / 128 * 2;   // whole stages
   const int64_t all = int64_t(p.vec_tiles) * p.row_tiles;
   p.splits = int(std::max<int64_t>(1, std::min<int64_t>({512 / all, p.chunks / 8, 32})));
   p.frags = align256(size_t(p.vec_tiles) * p.mt * p.chunks * pieces * kFrags * 1024);
@@ -738,7 +754,7 @@ Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   //   16 of fp16: 4096 x 4096 10.8 and 14.3, 8192 x 28672 52.0 and 63.6, 32000 x 4096 35.9 and 41.3
   //    8 of fp32: 4096 x 4096 10.5 and 15.1, 8192 x 28672 46.3 and 69.3, 32000 x 4096 23.6 and 43.0
   const int two = xtype == SEEDQ_F32 ? 8 : xtype == SEEDQ_F16 ? 16 : nrows * ncols <= int64_t(1) << 26 ? 32 : 16;
-  return nvec <= two ? Way::kBatch : Way::kMany;
+  return nvec <= two && ncols > 15 * kMxBlock ? Way::kBatch : Way::kMany;   // a batch reads 16 exponents
 }
 int pieces_of(int xtype) { return xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1; }
 

@@ -6,7 +6,7 @@
 #include <type_traits>
 
 #include "seedq_mx4_internal.h"
-#include "seedq_ops_device.h"
+#include "seedq_mx4_device.h"
 
 namespace seedq {
 namespace {
@@ -15,14 +15,6 @@ typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t uint32x2 __attribute__((ext_vector_type(2)));
-// Bytes anywhere.
-typedef uint32x2 uint32x2_byte __attribute__((aligned(1)));
-typedef uint32x4 uint32x4_byte __attribute__((aligned(1)));
-
-__device__ __forceinline__ void store_y(void* y, int ytype, int64_t at, float v) {
-  if (ytype == SEEDQ_F32) static_cast<float*>(y)[at] = v;
-  else static_cast<uint16_t*>(y)[at] = ytype == SEEDQ_F16 ? F16::narrow(v) : BF16::narrow(v);
-}
 
 constexpr int kFp4 = 4;   // the instructions' number for the type
 __device__ __forceinline__ intx8 fp4_operand(uint32x4 c) {
@@ -66,15 +58,7 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 #pragma unroll
     for (int d = 0; d < kStep; ++d)
       k.code[d] = *reinterpret_cast<const uint32x4*>(side.codes + std::min(b0 + 4 * d + kg, nblocks - 1) * 4);
-    if (b0 + 4 * kStep <= nblocks) {
-      k.s = *reinterpret_cast<const uint32x4_byte*>(side.scale + b0);
-    } else {
-#pragma unroll
-      for (int d = 0; d < kStep; ++d) {
-        const int64_t block = b0 + 4 * d + kg;
-        k.s[d] = block < nblocks ? uint32_t(side.scale[block]) << (8 * kg) : 0u;
-      }
-    }
+    k.s = *reinterpret_cast<const uint32x4_byte*>(side.scale + std::min(b0, nblocks - 16));   // nblocks >= 16
   };
   Side arow[AT];
 #pragma unroll
@@ -87,7 +71,11 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 #pragma unroll
     for (int t = 0; t < AT; ++t) load(arow[t], ka[buf][t], step);
   };
-  const auto use = [&](int buf) __attribute__((always_inline)) {
+  const auto use = [&](int buf, int64_t step) __attribute__((always_inline)) {
+    const int64_t before = (step + 1) * 16 - nblocks;   // in the last step the row's last 16
+    kb[buf].s = after_bytes(kb[buf].s, before);
+#pragma unroll
+    for (int t = 0; t < AT; ++t) ka[buf][t].s = after_bytes(ka[buf][t].s, before);
 #pragma unroll
     for (int d = 0; d < kStep; ++d) {
       const int sb = int(kb[buf].s[d] >> (8 * kg));
@@ -101,10 +89,10 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
   if (from < to) fetch(0, from);
   for (int64_t s = from; s < to; s += 2) {
     if (s + 1 < to) fetch(1, s + 1);
-    use(0);
+    use(0, s);
     if (s + 1 >= to) break;
     if (s + 2 < to) fetch(0, s + 2);
-    use(1);
+    use(1, s + 1);
   }
 #pragma unroll
   for (int t = 0; t < AT; ++t)
@@ -132,13 +120,8 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 // one register that the products pick their byte of.
 constexpr int kBlocks = 8;   // of a stage
 
-__device__ __forceinline__ void to_lds16(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from),
-                                   (__attribute__((address_space(3))) void*)(to), 16, 0, 0);
-}
-
-template <int MT, int NT, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2)
+template <int MT, int NT, int WM, int WN, bool SHORT>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
 tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict__ y, int ytype,
             int64_t ldy, float* __restrict__ partial) {
   constexpr int kWaves = WM * WN, kRowsA = 32 * MT * WM, kRowsB = 32 * NT * WN;
@@ -168,87 +151,113 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
     from[k] = r < kRowsA ? a.codes + std::min(i0 + r, a.nrows - 1) * a.row_words
                          : b.codes + std::min(j0 + r - kRowsA, b.nrows - 1) * b.row_words;
   }
-  const uint8_t* sfrom[MT + NT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t)
-    sfrom[t] = a.scale + std::min(i0 + (wm * MT + t) * 32 + n, a.nrows - 1) * nblocks;
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-    sfrom[MT + t] = b.scale + std::min(j0 + (wn * NT + t) * 32 + n, b.nrows - 1) * nblocks;
-  struct Scales {
-    uint32x2 s[MT + NT];
-  };
+  // Exponents go to LDS sixteen blocks, two stages, at a time, a row a lane: a load of few
+  // bytes of many rows costs as much as one of sixteen.
+  static_assert(kRowsA + kRowsB == 64 * kWaves, "a row a lane");
+  const int srow = wave * 64 + lane;
+  const uint8_t* sfrom = srow < kRowsA ? a.scale + std::min(i0 + srow, a.nrows - 1) * nblocks
+                                       : b.scale + std::min(j0 + srow - kRowsA, b.nrows - 1) * nblocks;
+  uint32x4* const lds_e = lds + 2 * (kRowsA + kRowsB) * 8;   // [2][kRowsA + kRowsB]
   // Past the last block: its codes again under exponent 0 on both sides, which is 2^-254.
-  const auto fetch = [&](int64_t stage, int buf, Scales& k) __attribute__((always_inline)) {
+  const auto exponents = [&](int64_t stage) __attribute__((always_inline)) {
     const int64_t b0 = stage * kBlocks;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      to_lds16(from[i] + std::min(b0 + block[i], nblocks - 1) * 4,
-               &lds[(buf * (kRowsA + kRowsB) + (i * kWaves + wave) * 8) * 8]);
-    if (b0 + kBlocks <= nblocks) {
-#pragma unroll
-      for (int t = 0; t < MT + NT; ++t) k.s[t] = *reinterpret_cast<const uint32x2_byte*>(sfrom[t] + b0);
+    if constexpr (SHORT) {   // a row is shorter than sixteen bytes
+      uint32x4 e = {0u, 0u, 0u, 0u};
+      for (int j = 0; j < int(nblocks); ++j) e[j >> 2] |= uint32_t(sfrom[j]) << (8 * (j & 3));
+      return e;
     } else {
-#pragma unroll
-      for (int t = 0; t < MT + NT; ++t) {
-        k.s[t] = uint32x2{0u, 0u};
-        for (int j = 0; j < kBlocks && b0 + j < nblocks; ++j)
-          k.s[t][j >> 2] |= uint32_t(sfrom[t][b0 + j]) << (8 * (j & 3));
-      }
+      return *reinterpret_cast<const uint32x4_byte*>(sfrom + std::min(b0, nblocks - 16));
     }
   };
+  const auto of_stage = [&](uint32x4 e, int64_t stage) __attribute__((always_inline)) {
+    return after_bytes(e, SHORT ? stage * kBlocks : stage * kBlocks + 16 - nblocks);
+  };
+  // The loads of a stage one by one.
+  const auto fetch = [&](int64_t stage, int buf, int i) __attribute__((always_inline)) {
+    to_lds16(from[i] + std::min(stage * kBlocks + block[i], nblocks - 1) * 4,
+             &lds[(buf * (kRowsA + kRowsB) + (i * kWaves + wave) * 8) * 8]);
+  };
   floatx16 acc[MT][NT] = {};
-  Scales cur;
-  fetch(s0, 0, cur);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) fetch(s0, 0, i);
+  lds_e[srow] = of_stage(exponents(s0), s0);
+  uint32x4 e = {0u, 0u, 0u, 0u};
   const uint32_t pick = kg ? 0x07050301u : 0x06040200u;   // blocks kg, 2 + kg, 4 + kg, 6 + kg
   const int swizzle = (n >> 1) & 7;
   for (int64_t s = s0; s < s1; ++s) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this stage's codes are in LDS
     __syncthreads();                                   // everybody's; the other buffer is free
     const int buf = int(s - s0) & 1;
-    Scales next = cur;
-    if (s + 1 < s1) fetch(s + 1, buf ^ 1, next);
+    const int64_t later = std::min(s + 1, s1 - 1);   // always, so that there is no branch
+    const int odd = int(s - s0) & 1, pair = int(s - s0) >> 1 & 1;
+    if (!odd && s + 2 < s1) e = exponents(s + 2);
+    if (odd) lds_e[(pair ^ 1) * (kRowsA + kRowsB) + srow] = of_stage(e, s + 1);   // read from the next barrier on
     int sc[MT + NT];
+    const uint32x2* le = reinterpret_cast<const uint32x2*>(lds_e + pair * (kRowsA + kRowsB)) + odd;
 #pragma unroll
-    for (int t = 0; t < MT + NT; ++t) sc[t] = int(__builtin_amdgcn_perm(cur.s[t][1], cur.s[t][0], pick));
+    for (int t = 0; t < MT + NT; ++t) {
+      const uint32x2 w = le[2 * (t < MT ? (wm * MT + t) * 32 + n : kRowsA + (wn * NT + t - MT) * 32 + n)];
+      sc[t] = int(__builtin_amdgcn_perm(w[1], w[0], pick));
+    }
     const uint32x4* la = lds + (buf * (kRowsA + kRowsB) + wm * MT * 32 + n) * 8;
     const uint32x4* lb = lds + (buf * (kRowsA + kRowsB) + kRowsA + wn * NT * 32 + n) * 8;
+    // The operands of a step of 64 columns are read between the products of the step before,
+    // in the order in which they are needed: left to itself the compiler reads them right
+    // before their use. The next stage's loads are issued one by one between the first products.
+    uint32x4 ca[2][MT], cb[2][NT];
+    const auto operand = [&](int k, int o) __attribute__((always_inline)) {
+      const int place = (2 * k + kg) ^ swizzle;
+      if (o < NT) cb[k & 1][o] = lb[o * 256 + place];
+      else ca[k & 1][o - NT] = la[(o - NT) * 256 + place];
+    };
     const auto products = [&](auto kk) __attribute__((always_inline)) {
       constexpr int K = decltype(kk)::value;
-      intx8 ca[MT], cb[NT];
-      const int place = (2 * K + kg) ^ swizzle;
-#pragma unroll
-      for (int t = 0; t < MT; ++t) ca[t] = fp4_operand(la[t * 256 + place]);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) cb[t] = fp4_operand(lb[t * 256 + place]);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ca[i], cb[j], acc[i][j], kFp4, kFp4,
-                                                                      K, sc[i], K, sc[MT + j]);
+        for (int j = 0; j < NT; ++j) {
+          constexpr int kGroups = 4 * MT * NT;   // the loads between the first half of the products
+          const int at = K * MT * NT + i * NT + j;
+          for (int l = at * 2 * kLoads / kGroups; l < (at + 1) * 2 * kLoads / kGroups; ++l)
+            if (l < kLoads) fetch(later, buf ^ 1, l);
+          if (K < 3 && i * NT + j < MT + NT) operand(K + 1, i * NT + j);
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+              fp4_operand(ca[K & 1][i]), fp4_operand(cb[K & 1][j]), acc[i][j], kFp4, kFp4, K, sc[i], K, sc[MT + j]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
     };
+    static_assert(MT * NT >= MT + NT, "an operand a product");
+#pragma unroll
+    for (int o = 0; o < MT + NT; ++o) operand(0, o);
     products(std::integral_constant<int, 0>{});
     products(std::integral_constant<int, 1>{});
     products(std::integral_constant<int, 2>{});
     products(std::integral_constant<int, 3>{});
-    cur = next;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way to LDS when it is given up
   // register e of lane l: row 8 (e / 4) + 4 (l / 32) + e % 4 of A, row l % 32 of B
+  const auto write = [&](auto type, void* to, int64_t ld) __attribute__((always_inline)) {
+    using Y = decltype(type);
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int64_t r = j0 + (wn * NT + j) * 32 + n;
-    if (r >= b.nrows) continue;
+    for (int j = 0; j < NT; ++j) {
+      const int64_t r = j0 + (wn * NT + j) * 32 + n;
+      if (r >= b.nrows) continue;
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+      for (int i = 0; i < MT; ++i) {
+        const int64_t v0 = i0 + (wm * MT + i) * 32 + 4 * kg;
+        typename Y::raw* p = static_cast<typename Y::raw*>(to) + v0 * ld + r;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t v = i0 + (wm * MT + i) * 32 + 8 * (e >> 2) + 4 * kg + (e & 3);
-        if (v >= a.nrows) continue;
-        if (splits > 1) partial[(split * a.nrows + v) * b.nrows + r] = acc[i][j][e];
-        else store_y(y, ytype, v * ldy + r, acc[i][j][e]);
+        for (int e = 0; e < 16; ++e) {
+          const int v = 8 * (e >> 2) + (e & 3);
+          if (v0 + v < a.nrows) p[v * ld] = Y::narrow(acc[i][j][e]);
+        }
       }
-  }
+    }
+  };
+  if (splits > 1) write(F32{}, partial + split * a.nrows * b.nrows, b.nrows);
+  else if (ytype == SEEDQ_F32) write(F32{}, y, ldy);
+  else if (ytype == SEEDQ_F16) write(F16{}, y, ldy);
+  else write(BF16{}, y, ldy);
 }
 
 // The splits of the columns added in order.
@@ -275,7 +284,7 @@ struct Plan {
 };
 Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
   Plan p{};
-  if (na <= kFewRows) {
+  if (na <= kFewRows && nblocks >= 16) {
     const int64_t steps = (nblocks + 4 * kStep - 1) / (4 * kStep);
     p.b_tiles = int((nb + 15) / 16);
     p.waves = int(std::min<int64_t>(kFewWaves, steps));
@@ -283,7 +292,7 @@ Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
   } else {
     const int64_t stages = (nblocks + kBlocks - 1) / kBlocks;
     const auto tiles = [&](int64_t t) { return ((na + t - 1) / t) * ((nb + t - 1) / t); };
-    p.tile = na > 128 && tiles(256) >= 256 ? 256 : 128;
+    p.tile = na > 128 && tiles(256) >= 256 && nblocks >= 16 ? 256 : 128;
     p.a_tiles = int((na + p.tile - 1) / p.tile), p.b_tiles = int((nb + p.tile - 1) / p.tile);
     p.splits = int(std::max<int64_t>(
         1, std::min<int64_t>({512 / (int64_t(p.a_tiles) * p.b_tiles), stages / 4, 16})));
@@ -313,11 +322,12 @@ hipError_t launch(const Mx4& a, const Mx4& b, void* d_y, int ytype, int64_t ldy,
   } else {
     const int64_t units = (int64_t(p.b_tiles) * p.splits + 7) / 8 * 8;
     auto go = [&](auto kern, int waves) {
-      hipLaunchKernelGGL(kern, dim3(unsigned(units * p.a_tiles)), dim3(64 * waves), size_t(4) * p.tile * 128,
+      hipLaunchKernelGGL(kern, dim3(unsigned(units * p.a_tiles)), dim3(64 * waves), size_t(4) * p.tile * (128 + 16),
                          stream, a, b, p.a_tiles, p.b_tiles, p.splits, d_y, ytype, ldy, partial);
     };
-    if (p.tile == 256) go(tile_kernel<4, 2, 2, 4>, 8);
-    else go(tile_kernel<2, 2, 2, 2>, 4);
+    if (b.nblocks < 16) go(tile_kernel<2, 2, 2, 2, true>, 4);
+    else if (p.tile == 256) go(tile_kernel<4, 2, 2, 4, false>, 8);
+    else go(tile_kernel<2, 2, 2, 2, false>, 4);
   }
   if (p.splits > 1)
     hipLaunchKernelGGL(join_kernel, dim3(unsigned((b.nrows + 255) / 256), unsigned(a.nrows)), dim3(256), 0,
