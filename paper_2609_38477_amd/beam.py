@@ -121,12 +121,10 @@ def beam_select(logits, scores, top: int, finished=None, pad_token: int = 0, str
     return BeamStep(score, parent, token)
 
 
-def _pieces(t):
-    """(row stride, pieces, stride of pieces, bytes of a piece) of the rows of t in bytes,
-    or None where a row is more than pieces at one stride."""
-    size = t.element_size()
-    inner, outer, step, i = size, 1, 0, t.dim() - 1
-    shape, stride = t.shape, t.stride()
+def _pieces(shape, stride, size: int):
+    """(row stride, pieces, stride of pieces, bytes of a piece) of rows in bytes, or None
+    where a row is more than pieces at one stride."""
+    inner, outer, step, i = size, 1, 0, len(shape) - 1
     while i > 0 and (shape[i] == 1 or stride[i] * size == inner):
         inner *= shape[i]
         i -= 1
@@ -142,6 +140,40 @@ def _pieces(t):
             outer *= shape[i]
         i -= 1
     return stride[0] * size, outer, step, inner
+
+
+def _split(a, b):
+    """a and b with the pieces of the one whose pieces are longer cut to the other's, or
+    None where they do not divide them."""
+    if a[3] == b[3]:
+        return a, b
+    if a[3] < b[3]:
+        other = _split(b, a)
+        return other and (other[1], other[0])
+    row, outer, step, inner = a
+    if inner % b[3] or (outer > 1 and step != inner):
+        return None
+    return (row, outer * (inner // b[3]), b[3], b[3]), b
+
+
+@functools.lru_cache(maxsize=1024)
+def _moved(shape, stride, to_stride, size: int):
+    """How rows of one layout go to another: (source's and destination's row stride,
+    source's and destination's stride of pieces, pieces, bytes of a piece), or None;
+    to_stride None for dense rows."""
+    src = _pieces(shape, stride, size)
+    if to_stride is None:
+        n = size
+        for k in shape[1:]:
+            n *= k
+        dst = (n, 1, 0, n)
+    else:
+        dst = _pieces(shape, to_stride, size)
+    both = src and dst and _split(src, dst)
+    if not both:
+        return None
+    src, dst = both
+    return src[0], dst[0], src[2], dst[2], src[1], src[3]
 
 
 def beam_reorder(states, parents, out=None, stream=None):
@@ -169,61 +201,44 @@ def beam_reorder(states, parents, out=None, stream=None):
         out = [out] if isinstance(out, torch.Tensor) else list(out)
         if len(out) != len(states):
             raise ValueError(f"out: {len(states)} tensors wanted, not {len(out)}")
-    beams = None
+    rows = states[0].shape[0] if states and states[0].dim() else 0
+    beams = rows // batch if batch else 1
+    if states and (rows != batch * beams or not 1 <= beams <= SEEDQ_MAX_BEAMS):
+        raise ValueError(f"states: rows of {batch} sequences of 1 to {SEEDQ_MAX_BEAMS} beams wanted, "
+                         f"not {rows}")
+    out_rows = batch * out_beams
     with _on(stream):
-        results, keep = [], []
-        array = (BeamState * len(states))()
+        results, fields, keep = [], [], []
         for k, s in enumerate(states):
-            if s.dim() < 1 or s.get_device() != device:
-                raise ValueError(f"states: tensors of rows on GPU {device} wanted, not "
-                                 f"{tuple(s.shape)} on {s.device}")
-            rows = s.shape[0]
-            if beams is None:
-                beams = rows // batch if batch else 1
-            if rows != batch * beams or not 1 <= beams <= SEEDQ_MAX_BEAMS:
-                raise ValueError(f"states: rows of {batch} sequences of 1 to {SEEDQ_MAX_BEAMS} beams "
-                                 f"wanted, not {rows}")
-            shape = (batch * out_beams, *s.shape[1:])
+            shape = s.shape
+            if not shape or shape[0] != rows or s.get_device() != device:
+                raise ValueError(f"states: tensors of {rows} rows on GPU {device} wanted, not "
+                                 f"{tuple(shape)} on {s.device}")
             if out is None:
-                o = s.new_empty(shape)
+                o, to = s.new_empty((out_rows, *shape[1:])), None
             else:
                 o = out[k]
-                if o.dtype != s.dtype or o.shape != shape or o.get_device() != device:
-                    raise ValueError(f"out: {s.dtype} of shape {shape} on GPU {device} wanted, not "
-                                     f"{o.dtype} {tuple(o.shape)} on {o.device}")
+                if o.dtype != s.dtype or o.shape != (out_rows, *shape[1:]) or o.get_device() != device:
+                    raise ValueError(f"out: {s.dtype} of shape {(out_rows, *shape[1:])} on GPU {device} "
+                                     f"wanted, not {o.dtype} {tuple(o.shape)} on {o.device}")
+                to = o.stride()
+                if _pieces(o.shape, to, 1) is None:
+                    raise ValueError("out: rows that are pieces at one stride wanted")
             results.append(o)
-            if s.numel() == 0 or o.numel() == 0:
+            at, to_at = s.data_ptr(), o.data_ptr()
+            if not at or not to_at:   # no elements
                 continue
-            src, dst = _pieces(s), _pieces(o)
-            if dst is None:
-                raise ValueError("out: rows that are pieces at one stride wanted")
-            if o.data_ptr() == s.data_ptr() and (src != dst or out_beams != beams):
+            if at == to_at and (s.stride() != to or out_beams != beams):
                 raise ValueError("out: in place, the states' own layout and number of beams wanted")
-            if src is None or (src[1], src[3]) != (dst[1], dst[3]):
-                if out is not None and src is not None:
-                    src, dst = _split(src, dst)
-                else:
-                    s = s.contiguous()
-                    keep.append(s)
-                    src = _pieces(s)
-                    src, dst = _split(src, dst)
-            if src is None:
-                raise ValueError("out: pieces that divide the states' or are divided by them wanted")
-            array[k] = BeamState(s.data_ptr(), o.data_ptr(), src[0], dst[0], src[2], dst[2], src[1],
-                                 src[3])
-        _check(lib().seedq_beam_reorder(array, len(states), parents.data_ptr(), batch, beams or 1,
-                                        out_beams, _handle(device)), "seedq_beam_reorder")
+            moved = _moved(shape, s.stride(), to, s.element_size())
+            if moved is None:
+                s = s.contiguous()
+                keep.append(s)
+                at, moved = s.data_ptr(), _moved(shape, s.stride(), to, s.element_size())
+            fields += (at, to_at, *moved)
+        if fields:
+            array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
+            _check(lib().seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,
+                                            out_beams, _handle(device)), "seedq_beam_reorder")
     return results[0] if single else results
 
-
-def _split(a, b):
-    """a and b with the pieces of the one whose pieces are longer cut to the other's."""
-    if a[3] < b[3]:
-        b, a = _split(b, a)
-        return a, b
-    row, outer, step, inner = a
-    if inner == b[3]:
-        return a, b
-    if inner % b[3] or (outer > 1 and step != inner):
-        return None, None
-    return (row, outer * (inner // b[3]), b[3], b[3]), b

@@ -130,8 +130,8 @@ struct Offer {
   uint32_t beam;
   Key key;
   __device__ __forceinline__ bool before(const Offer& o) const {
-    if (total != o.total) return total > o.total;
-    return beam != o.beam ? beam < o.beam : key > o.key;
+    return (total > o.total) |
+           ((total == o.total) & ((beam < o.beam) | ((beam == o.beam) & (key > o.key))));
   }
 };
 __device__ __forceinline__ uint64_t order_of(double v) {
@@ -148,33 +148,57 @@ __device__ __forceinline__ double total_of(uint64_t k) {
 // `top` in all.
 constexpr int kJoinThreads = 256;
 constexpr int kMaxLists = kMaxBeams * kMaxSegs;
+constexpr int kAhead = 2;    // keys of a thread that are read at once
 __global__ void __launch_bounds__(kJoinThreads)
 beam_join_kernel(BeamArgs a, int segs, const Partial* __restrict__ partial,
                  const Key* __restrict__ seg_top) {
   enum { kNone, kTokens, kFinished, kBad };
-  __shared__ double far[kMaxBeams];    // m + log S, and in two parts: m
-  __shared__ double log_s[kMaxBeams];
+  __shared__ double most[kMaxBeams], log_s[kMaxBeams];
   __shared__ float score[kMaxBeams];
-  __shared__ int kind[kMaxBeams], bad, n, any_bound;
+  __shared__ int kind[kMaxBeams], bad, n, none;
+  __shared__ Partial part[kMaxLists];
   __shared__ Offer list[kMaxTop * kMaxTop], bound, first[kMaxLists], last[kMaxTop];
   const int tid = int(threadIdx.x);
   const int64_t i = blockIdx.x, t0 = i * a.beams;
-  if (tid == 0) bad = n = any_bound = 0;
+  const int lists = a.beams * segs, keys = lists * a.top;
+  const bool many = lists >= a.top;
+  const int deep = many ? 0 : (a.top + lists - 1) / lists - 1;
+  const Key* in = seg_top + t0 * segs * a.top;
+  // Everything that the first kernel left is asked for before anything is waited for. What
+  // beams without tokens left in its place is not looked at.
+  Key ahead[kAhead], head[kMaxLists / kJoinThreads], tail = 0;
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (tid + k * kJoinThreads < keys) ahead[k] = in[tid + k * kJoinThreads];
+#pragma unroll
+  for (int k = 0; k < kMaxLists / kJoinThreads; ++k) {
+    const int l = tid + k * kJoinThreads;
+    if (l < lists) {
+      head[k] = in[l * a.top + deep];
+      part[l] = partial[t0 * segs + l];
+    }
+  }
+  if (!many && tid < lists) tail = in[tid * a.top + a.top - 1];
+  float s = -kInf;
+  bool done = false;
+  if (tid < a.beams) {
+    s = a.scores[t0 + tid];
+    done = a.finished && a.finished[t0 + tid];
+  }
+  if (tid == 0) bad = n = none = 0;
   __syncthreads();
   if (tid < a.beams) {
-    const int64_t t = t0 + tid;
-    const float s = a.scores[t];
     int k = kNone;
     if (!(s < kInf)) k = kBad;
-    else if (s > -kInf && a.finished && a.finished[t]) k = kFinished;
+    else if (s > -kInf && done) k = kFinished;
     else if (s > -kInf) {
-      const Partial* p = partial + t * segs;
+      const Partial* p = part + tid * segs;
       float m = p[0].m;
       for (int g = 1; g < segs; ++g) m = fmaxf(m, p[g].m);
       double S = 0.0;
       for (int g = 0; g < segs; ++g)
         S += double(__builtin_amdgcn_exp2f(fmaxf(p[g].m - m, kFar) * kLog2E)) * p[g].S;
-      far[tid] = m;
+      most[tid] = m;
       log_s[tid] = log(S);
       k = S > 0.0 ? kTokens : S == 0.0 ? kNone : kBad;
     }
@@ -191,69 +215,73 @@ beam_join_kernel(BeamArgs a, int segs, const Partial* __restrict__ partial,
     }
     return;
   }
-  const int lists = a.beams * segs;
-  const auto offer = [&](int l, int pos) {
+  // Offer `pos` of list l, whose key is `key` if it is one of a token.
+  const auto offer = [&](int l, int pos, Key key) {
     const uint32_t b = uint32_t(l / segs);
     Offer o{0, b, 0};
-    if (kind[b] == kTokens) {
-      o.key = seg_top[(t0 * segs + l) * a.top + pos];
-      if (o.key) o.total = order_of(double(score[b]) + ((double(key_value(o.key)) - far[b]) - log_s[b]));
+    if (kind[b] == kTokens && key) {
+      o.key = key;
+      o.total = order_of(double(score[b]) + ((double(key_value(key)) - most[b]) - log_s[b]));
     } else if (kind[b] == kFinished && l % segs == 0 && pos == 0) {
       o.key = 1;
       o.total = order_of(double(score[b]));
     }
     return o;
   };
-  const bool many = lists >= a.top;
-  const int deep = many ? 0 : (a.top + lists - 1) / lists - 1;
-  for (int l = tid; l < lists; l += kJoinThreads) {
-    first[l] = offer(l, deep);
-    if (many) continue;
-    last[l] = offer(l, a.top - 1);
-    if (first[l].total == 0) any_bound = -1;   // the worst of them is none
+#pragma unroll
+  for (int k = 0; k < kMaxLists / kJoinThreads; ++k) {
+    const int l = tid + k * kJoinThreads;
+    if (l < lists) {
+      first[l] = offer(l, deep, head[k]);
+      if (!many && first[l].total == 0) none = 1;   // the worst of them is none
+    }
   }
+  if (!many && tid < lists) last[tid] = offer(tid, a.top - 1, tail);
+  if (tid == 0) bound = Offer{0, 0, 0};
   __syncthreads();
+  // A bound that is no offer cuts nothing: every offer stands before it.
   if (many) {
-    for (int l = tid; l < lists; l += kJoinThreads) {
+#pragma unroll
+    for (int k = 0; k < kMaxLists / kJoinThreads; ++k) {
+      const int l = tid + k * kJoinThreads;
+      if (l >= lists) continue;
       const Offer mine = first[l];
       int rank = 0;
+#pragma unroll 4
       for (int j = 0; j < lists; ++j) rank += first[j].before(mine) ? 1 : 0;
-      if (rank == a.top - 1 && mine.total) {
-        bound = mine;
-        any_bound = 1;
-      }
+      if (rank == a.top - 1 && mine.total) bound = mine;
     }
-  } else if (tid == 0) {
-    Offer worst = first[0];
-    for (int l = 1; l < lists; ++l)
-      if (worst.before(first[l])) worst = first[l];
-    Offer lowest = worst;
-    bool some = any_bound == 0;
-    for (int l = 0; l < lists; ++l) {
-      if (last[l].total && (!some || last[l].before(lowest))) {
-        lowest = last[l];
-        some = true;
-      }
+  } else if (tid < lists) {
+    // the worst of the first ones, if all are offers, and the best of the last ones
+    const Offer mine = first[tid], end = last[tid];
+    int worse = 0, better = 0;
+#pragma unroll 4
+    for (int j = 0; j < lists; ++j) {
+      worse += mine.before(first[j]) ? 1 : 0;
+      better += last[j].before(end) ? 1 : 0;
     }
-    bound = lowest;
-    any_bound = some ? 1 : 0;
+    if (better == 0 && end.total) bound = end;
+    if (worse == 0 && !none) list[0] = mine;
   }
   __syncthreads();
-  const bool cut = any_bound == 1;
-  for (int k = tid; k < lists * a.top; k += kJoinThreads) {
-    const int l = k / a.top;
-    if (many && cut && bound.before(first[l])) continue;   // the whole list lies below
-    const Offer o = offer(l, k % a.top);
-    if (o.total && !(cut && bound.before(o))) {
-      const int at = atomicAdd(&n, 1);
-      list[at] = o;
-    }
+  Offer cut = bound;
+  if (!many && !none && list[0].before(cut)) cut = list[0];
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k * kJoinThreads < keys; ++k) {
+    const int at = tid + k * kJoinThreads;
+    if (at >= keys) break;
+    const int l = at / a.top;
+    if (many && cut.before(first[l])) continue;   // the whole list lies below
+    const Offer o = offer(l, at % a.top, k == 0 ? ahead[0] : k == 1 ? ahead[1] : in[at]);
+    if (o.total && !cut.before(o)) list[atomicAdd(&n, 1)] = o;
   }
   __syncthreads();
   const int count = n;
   for (int k = tid; k < count; k += kJoinThreads) {
     const Offer mine = list[k];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < count; ++j) rank += list[j].before(mine) ? 1 : 0;
     if (rank >= a.top) continue;
     a.score[out + rank] = float(total_of(mine.total));
@@ -303,49 +331,80 @@ struct States {
 static_assert(sizeof(States) <= 3584, "fits the kernel's arguments");
 constexpr int kMoveThreads = 256;
 
+// A number at any byte, and 16 bytes.
+template <class T>
+struct __attribute__((packed)) Packed {
+  T v;
+};
+typedef uint32x4 uint32x4_byte __attribute__((aligned(1)));
+
+// One unit of every row of a sequence.
 template <int NB>
-__global__ void __launch_bounds__(kMoveThreads)
-reorder_kernel(States all, const int64_t* __restrict__ parent, int in_beams, int out_beams) {
-  const int64_t seq = blockIdx.y;
-  int which = 0;   // the last whose first block is not past this one
-  for (int step = 32; step > 0; step >>= 1)
-    if (which + step < all.n && blockIdx.x >= all.s[which + step].first_block) which += step;
-  const State& s = all.s[which];
-  const uint32_t u = (blockIdx.x - s.first_block) * kMoveThreads + threadIdx.x;
-  if (u >= s.units) return;
+__device__ __forceinline__ void move_unit(const State& s, const char* src, char* dst, uint32_t u,
+                                          const int64_t* par, int in_beams, int out_beams) {
   const uint32_t piece = u / s.per_piece;
   const int64_t at = int64_t(u - piece * s.per_piece) * 16;
-  const char* src = s.src + seq * in_beams * s.src_row + piece * s.src_outer + at;
-  char* dst = s.dst + seq * out_beams * s.dst_row + piece * s.dst_outer + at;
-  const int64_t* par = parent + seq * out_beams;
+  src += piece * s.src_outer + at;
+  dst += piece * s.dst_outer + at;
   const int64_t left = s.inner - at;
   const auto from = [&](int j) { return par[j] >= 0 && par[j] < in_beams ? par[j] : int64_t(-1); };
+  const auto stays = [&](int j) { return s.in_place && par[j] == j; };
   if (left >= 16) {
     uint32x4 v[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       v[j] = uint32x4{0u, 0u, 0u, 0u};
-      if (j < out_beams) {
-        const int64_t p = from(j);
-        if (p >= 0 && !(s.in_place && p == j)) v[j] = load16(src + p * s.src_row);
+      if (j < out_beams && from(j) >= 0 && !stays(j)) v[j] = *reinterpret_cast<const uint32x4_byte*>(src + from(j) * s.src_row);
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (j < out_beams && !stays(j)) *reinterpret_cast<uint32x4_byte*>(dst + j * s.dst_row) = v[j];
+  } else {   // the piece's end, by the bits of its length
+    Packed<uint64_t> v8[NB];
+    Packed<uint32_t> v4[NB];
+    Packed<uint16_t> v2[NB];
+    uint8_t v1[NB];
+    const int n = int(left), at4 = n & 8, at2 = n & 12, at1 = n & 14;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      v8[j].v = 0, v4[j].v = 0, v2[j].v = 0, v1[j] = 0;
+      if (j < out_beams && from(j) >= 0 && !stays(j)) {
+        const char* p = src + from(j) * s.src_row;
+        if (n & 8) v8[j] = *reinterpret_cast<const Packed<uint64_t>*>(p);
+        if (n & 4) v4[j] = *reinterpret_cast<const Packed<uint32_t>*>(p + at4);
+        if (n & 2) v2[j] = *reinterpret_cast<const Packed<uint16_t>*>(p + at2);
+        if (n & 1) v1[j] = uint8_t(p[at1]);
       }
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      if (j < out_beams && !(s.in_place && par[j] == j)) store16(dst + j * s.dst_row, v[j]);
-  } else {
-    for (int64_t b = 0; b < left; ++b) {
-      char v[NB];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        v[j] = 0;
-        if (j < out_beams && from(j) >= 0 && !(s.in_place && par[j] == j))
-          v[j] = src[from(j) * s.src_row + b];
+      if (j < out_beams && !stays(j)) {
+        char* p = dst + j * s.dst_row;
+        if (n & 8) *reinterpret_cast<Packed<uint64_t>*>(p) = v8[j];
+        if (n & 4) *reinterpret_cast<Packed<uint32_t>*>(p + at4) = v4[j];
+        if (n & 2) *reinterpret_cast<Packed<uint16_t>*>(p + at2) = v2[j];
+        if (n & 1) p[at1] = char(v1[j]);
       }
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-        if (j < out_beams && !(s.in_place && par[j] == j)) dst[j * s.dst_row + b] = v[j];
-    }
+  }
+}
+
+// A workgroup takes `each` x kMoveThreads neighbouring units of a tensor.
+template <int NB>
+__global__ void __launch_bounds__(kMoveThreads)
+reorder_kernel(States all, int each, const int64_t* __restrict__ parent, int in_beams, int out_beams) {
+  const int64_t seq = blockIdx.y;
+  int which = 0;   // the last whose first block is not past this one
+  for (int step = 32; step > 0; step >>= 1)
+    if (which + step < all.n && blockIdx.x >= all.s[which + step].first_block) which += step;
+  const State s = all.s[which];
+  const char* src = s.src + seq * in_beams * s.src_row;
+  char* dst = s.dst + seq * out_beams * s.dst_row;
+  const uint32_t u0 = (blockIdx.x - s.first_block) * uint32_t(each * kMoveThreads) + threadIdx.x;
+#pragma unroll 1
+  for (int k = 0; k < each; ++k) {
+    const uint32_t u = u0 + k * kMoveThreads;
+    if (u >= s.units) break;
+    move_unit<NB>(s, src, dst, u, parent + seq * out_beams, in_beams, out_beams);
   }
 }
 
@@ -389,6 +448,10 @@ hipError_t launch_beam_select(const BeamArgs& all, int type, void* d_ws, hipStre
 hipError_t launch_beam_reorder(const seedq_beam_state* states, int64_t nstates, const int64_t* d_parent,
                                int64_t batch, int in_beams, int out_beams, hipStream_t stream) {
   constexpr int64_t kMaxBlocks = int64_t(1) << 23;   // of a launch's grid
+  // Units of a thread: few where there is little to move, so that every CU has some.
+  double units = 0;
+  for (int64_t i = 0; i < nstates; ++i) units += double(states[i].outer) * double(states[i].inner) / 16;
+  const int each = int(std::max(1.0, std::min(8.0, units * double(batch) / (kMoveThreads * 2048.0))));
   States all;
   all.n = 0;
   int64_t blocks = 0;
@@ -401,8 +464,8 @@ hipError_t launch_beam_reorder(const seedq_beam_state* states, int64_t nstates, 
       }
       const dim3 grid(unsigned(blocks), unsigned(std::min<int64_t>(batch - b, 65535)));
       auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, grid, dim3(kMoveThreads), 0, stream, part, d_parent + b * out_beams,
-                           in_beams, out_beams);
+        hipLaunchKernelGGL(kern, grid, dim3(kMoveThreads), 0, stream, part, each,
+                           d_parent + b * out_beams, in_beams, out_beams);
       };
       if (out_beams <= 4) go(reorder_kernel<4>);
       else if (out_beams <= 8) go(reorder_kernel<8>);
@@ -427,7 +490,7 @@ hipError_t launch_beam_reorder(const seedq_beam_state* states, int64_t nstates, 
         State e = d;
         e.src += o * s.src_outer + at, e.dst += o * s.dst_outer + at;
         e.inner = len, e.per_piece = uint32_t(per), e.units = uint32_t(per * take);
-        const int64_t need = (int64_t(e.units) + kMoveThreads - 1) / kMoveThreads;
+        const int64_t need = (int64_t(e.units) + each * kMoveThreads - 1) / (each * kMoveThreads);
         if (all.n == kStates || blocks + need > kMaxBlocks) flush();
         e.first_block = uint32_t(blocks);
         all.s[all.n++] = e;

@@ -164,18 +164,26 @@ def test_helpers_refuse_tensors_on_the_host(sq):
 
 def test_pieces_of_rows(sq):
     import torch
-    from paper_2609_38477_amd.beam import _pieces, _split
+    from paper_2609_38477_amd.beam import _moved, _pieces, _split
+
+    def pieces(t):
+        return _pieces(t.shape, t.stride(), t.element_size())
+
     t = torch.zeros(4, 3, 10, 8)
-    assert _pieces(t) == (960, 1, 0, 960)
-    assert _pieces(t[:, :, :7]) == (960, 3, 320, 224)
-    assert _pieces(t[:, :, 2:7, :5]) is None
-    assert _pieces(t[:, 1, :, 3]) == (960, 10, 32, 4)
-    assert _pieces(t[:, 1:2, 3, :]) == (960, 1, 0, 32)
-    assert _pieces(t.transpose(1, 2)) is None
-    assert _pieces(torch.zeros(5, dtype=torch.int64)) == (8, 1, 0, 8)
-    a, b = _split(_pieces(t[:, :, :7]), (672, 1, 0, 672))
+    assert pieces(t) == (960, 1, 0, 960)
+    assert pieces(t[:, :, :7]) == (960, 3, 320, 224)
+    assert pieces(t[:, :, 2:7, :5]) is None
+    assert pieces(t[:, 1, :, 3]) == (960, 10, 32, 4)
+    assert pieces(t[:, 1:2, 3, :]) == (960, 1, 0, 32)
+    assert pieces(t.transpose(1, 2)) is None
+    assert pieces(torch.zeros(5, dtype=torch.int64)) == (8, 1, 0, 8)
+    a, b = _split(pieces(t[:, :, :7]), (672, 1, 0, 672))
     assert a == (960, 3, 320, 224) and b == (672, 3, 224, 224)
-    assert _split((64, 2, 32, 12), (64, 3, 20, 8)) == (None, None)
+    assert _split((64, 2, 32, 12), (64, 3, 20, 8)) is None
+    view = t[:, :, :7]
+    assert _moved(view.shape, view.stride(), None, 4) == (960, 672, 320, 224, 3, 224)
+    assert _moved(view.shape, view.stride(), view.stride(), 4) == (960, 960, 320, 320, 3, 224)
+    assert _moved(t.shape, t.transpose(1, 2).stride(), None, 4) is None
 
 
 # ---------------------------------------------------------------- the oracle's definitions
