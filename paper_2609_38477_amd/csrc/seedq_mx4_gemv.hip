@@ -623,9 +623,9 @@ gemm_kernel(Mx4 q, int64_t nvec, const uint32x4* __restrict__ frags, int64_t chu
   else write(BF16{}, y, ldy);
 }
 
-constexpr int kPanelBytes = 96 << 10;
 constexpr size_t kLdsBytes = 160 << 10;
 constexpr int kWorkgroups = 256;
+constexpr int kMaxPanels = 32;
 
 struct BatchPlan {
   Cut cut;
@@ -633,35 +633,53 @@ struct BatchPlan {
   unsigned grid;
   size_t lds, partial;
 };
+// The cut that the following model finds fastest, in us. A wave goes through its chunks at
+// its share of the memory's rate, 1 KB RT in 0.84 RT with all waves at work, but no faster
+// than its loads in flight allow; a workgroup lays out its panel; panels cost a second
+// launch and its traffic.
 BatchPlan batch_plan(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   const int pieces = xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1;
   const int each = xtype == SEEDQ_F32 ? 4 : xtype == SEEDQ_F16 ? 8 : 16;
-  BatchPlan p;
-  p.xt = nvec <= each ? 1 : 2;
-  p.rt = p.xt == 1 ? 1 : 2;
+  BatchPlan best{};
+  const int xt = nvec <= each ? 1 : 2, rt = xt;
+  const int most = xt == 1 ? 16 : 8;
   const int64_t chunk_bytes = int64_t(pieces) * nvec * 256;
-  p.cut.chunks = int((ncols + kChunk - 1) / kChunk);
-  const int64_t tiles = (nrows + 16 * p.rt - 1) / (16 * p.rt);
-  // a workgroup's share of the codes, four times what it lays out in LDS for it
-  const int64_t share = tiles * 16 * p.rt * p.cut.chunks * 64 / kWorkgroups;
-  int64_t panels = (p.cut.chunks * chunk_bytes + kPanelBytes - 1) / kPanelBytes;
-  panels = std::max(panels, std::min<int64_t>(p.cut.chunks * chunk_bytes * 2 / std::max<int64_t>(share, 1), 16));
-  panels = std::max<int64_t>(1, std::min<int64_t>(panels, p.cut.chunks));
-  p.cut.panel_chunks = int((p.cut.chunks + panels - 1) / panels);
-  p.panels = (p.cut.chunks + p.cut.panel_chunks - 1) / p.cut.panel_chunks;
-  p.waves = p.xt == 1 ? 16 : 8;
-  const int64_t per_panel = std::max(1, kWorkgroups / p.panels);
-  p.cut.groups = int(std::max<int64_t>(1, std::min<int64_t>(p.waves, (tiles + per_panel - 1) / per_panel)));
-  p.cut.slices = std::max(1, std::min(p.waves / p.cut.groups, (p.cut.panel_chunks + kDeep - 1) / kDeep));
-  const size_t part = size_t(p.xt) * p.rt * 1024 * each / 16;   // of a wave, where slices meet
-  while (p.cut.slices > 1 && p.cut.panel_chunks * chunk_bytes + p.cut.groups * p.cut.slices * part > kLdsBytes)
-    --p.cut.slices;
-  p.waves = p.cut.groups * p.cut.slices;
-  p.grid = unsigned(std::min<int64_t>((tiles + p.cut.groups - 1) / p.cut.groups, 2 * per_panel));
-  p.lds = size_t(p.cut.panel_chunks) * chunk_bytes;
-  if (p.cut.slices > 1) p.lds += p.waves * part;
-  p.partial = p.panels > 1 ? align256(size_t(p.panels) * nvec * nrows * sizeof(float)) : 0;
-  return p;
+  const int chunks = int((ncols + kChunk - 1) / kChunk);
+  const int64_t tiles = (nrows + 16 * rt - 1) / (16 * rt);
+  const size_t part = size_t(xt) * rt * 1024 * each / 16;   // of a wave, where slices meet
+  double least = 0.0;
+  const auto consider = [&](int panels, int groups) {
+    BatchPlan p;
+    p.cut.chunks = chunks;
+    p.cut.panel_chunks = (chunks + panels - 1) / panels;
+    p.panels = (chunks + p.cut.panel_chunks - 1) / p.cut.panel_chunks;
+    const int steps = (p.cut.panel_chunks + kDeep - 1) / kDeep;
+    const int64_t per_panel = std::max(1, kWorkgroups / p.panels);
+    p.cut.groups = groups;
+    p.cut.slices = std::max(1, std::min(most / groups, steps));
+    p.waves = groups * p.cut.slices;
+    p.lds = p.cut.panel_chunks * chunk_bytes + (p.cut.slices > 1 ? p.waves * part : 0);
+    if (p.lds > kLdsBytes) return;
+    const int64_t units = (tiles + groups - 1) / groups;
+    p.grid = unsigned(std::min(units, per_panel));
+    const double rounds = double((units + p.grid - 1) / p.grid);
+    const double busy = double(p.grid) * p.panels * p.waves / (kWorkgroups * 16.0);
+    const double chunk = std::max({0.3, 0.84 * rt * busy, 0.7 * rt * p.waves / 16});
+    const double us = rounds * (((steps + p.cut.slices - 1) / p.cut.slices) * kDeep * chunk +
+                                (p.cut.slices > 1 ? 0.8 : 0.4)) +
+                      p.cut.panel_chunks * chunk_bytes / 6e4 +
+                      (p.panels > 1 ? 2.5 + p.panels * double(nvec) * nrows * 8 / 5e6 : 0.0);
+    if (best.panels && us >= least) return;
+    least = us;
+    p.xt = xt, p.rt = rt;
+    p.partial = p.panels > 1 ? align256(size_t(p.panels) * nvec * nrows * sizeof(float)) : 0;
+    best = p;
+  };
+  const int fit = int(std::max<int64_t>(1, (chunks * chunk_bytes + (128 << 10) - 1) / (128 << 10)));
+  for (int panels : {1, 2, 4, 8, 16, 32, fit, fit + 1, fit + 2})
+    if (panels >= fit && panels <= std::max(fit, std::min(kMaxPanels, chunks)))
+      for (int groups = 1; groups <= most; groups *= 2) consider(panels, groups);
+  return best;
 }
 
 template <class X>
@@ -743,17 +761,18 @@ hipError_t launch_gemm(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx,
 constexpr int64_t kMaxVecs = 32768;
 enum class Way { kFew, kBatch, kMany };
 Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
-  // The vector ALU takes two vectors, and four where rows are few: us by it and by a batch
-  //   2 of bf16: 4096 x 4096 5.0 and 6.0, 8192 x 28672 27.8 and 34, 32000 x 4096 18.4 and 17
-  //   4 of bf16: 4096 x 4096 6.4 and 8.2, 8192 x 28672 35.0 and 41.9, 14336 x 4096 14.9 and 11.4
-  //   4 of fp32: 4096 x 4096 8.8 and 10.0, 8192 x 28672 45.8 and 34.3
-  const bool small = nrows <= 8192 && (xtype != SEEDQ_F32 || nrows * ncols <= int64_t(1) << 25);
-  if (nvec <= (small ? 4 : 2)) return Way::kFew;
+  // The vector ALU takes two vectors, and up to four short ones where rows are few: us by it
+  // and by a batch
+  //   2 of bf16: 4096 x 4096 5.0 and 6.0, 8192 x 28672 27.8 and 31, 32000 x 4096 18.4 and 16.8
+  //   4 of bf16: 4096 x 4096 6.4 and 6.8, 8192 x 28672 35.0 and 31.8, 14336 x 4096 14.9 and 11.4
+  //   4 of fp32: 4096 x 4096 8.8 and 7.9, 2000 x 8192 18.4 and 8.4, 8192 x 28672 45.8 and 34.3
+  const int size = xtype == SEEDQ_F32 ? 4 : 2;
+  if (nvec <= 2 || (nvec <= 4 && nrows <= 8192 && nvec * ncols * size <= 48 << 10)) return Way::kFew;
   // A batch takes two tiles: us by it and by the tiles for many
-  //   32 of bf16: 4096 x 4096 11.8 and 13.6, 8192 x 28672 58.1 and 56.1, 32000 x 4096 40.9 and 36.8
-  //   16 of fp16: 4096 x 4096 10.8 and 14.3, 8192 x 28672 52.0 and 63.6, 32000 x 4096 35.9 and 41.3
-  //    8 of fp32: 4096 x 4096 10.5 and 15.1, 8192 x 28672 46.3 and 69.3, 32000 x 4096 23.6 and 43.0
-  const int two = xtype == SEEDQ_F32 ? 8 : xtype == SEEDQ_F16 ? 16 : nrows * ncols <= int64_t(1) << 26 ? 32 : 16;
+  //   32 of bf16: 4096 x 4096 11.4 and 13.6, 8192 x 28672 45.9 and 53.3, 32000 x 4096 30.5 and 35.5
+  //   16 of fp16: 4096 x 4096 9.6 and 14.3, 8192 x 28672 42.1 and 63.6, 32000 x 4096 26.1 and 41.3
+  //    8 of fp32: 4096 x 4096 8.6 and 15.1, 8192 x 28672 38.9 and 69.3, 32000 x 4096 24.1 and 43.0
+  const int two = xtype == SEEDQ_F32 ? 8 : xtype == SEEDQ_F16 ? 16 : 32;
   return nvec <= two && ncols > 15 * kMxBlock ? Way::kBatch : Way::kMany;   // a batch reads 16 exponents
 }
 int pieces_of(int xtype) { return xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1; }
