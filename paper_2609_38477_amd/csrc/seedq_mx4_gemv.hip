@@ -599,7 +599,7 @@ gemm_kernel(Mx4 q, int64_t nvec, const uint32x4* __restrict__ frags, int64_t chu
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way to LDS when it is given up
   // register i of lane l: vector 8 (i / 4) + 4 (l / 32) + i % 4, row l % 32
-  const auto write = [&](auto type, void* to, int64_t ld) __attribute__((always_inline)) {
+  const auto write = [&](auto type, auto whole, void* to, int64_t ld) __attribute__((always_inline)) {
     using Y = decltype(type);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -611,16 +611,21 @@ gemm_kernel(Mx4 q, int64_t nvec, const uint32x4* __restrict__ frags, int64_t chu
         typename Y::raw* p = static_cast<typename Y::raw*>(to) + v0 * ld + r;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int v = 8 * (i >> 2) + (i & 3);
-          if (v0 + v < nvec) p[v * ld] = Y::narrow(acc[t][m][i]);
+          if (decltype(whole)::value || v0 + 8 * (i >> 2) + (i & 3) < nvec) *p = Y::narrow(acc[t][m][i]);
+          p += (i & 3) == 3 ? 5 * ld : ld;
+          __builtin_amdgcn_sched_barrier(0);   // one address at a time
         }
       }
     }
   };
-  if (splits > 1) write(F32{}, partial + split * nvec * q.nrows, q.nrows);
-  else if (ytype == SEEDQ_F32) write(F32{}, y, ldy);
-  else if (ytype == SEEDQ_F16) write(F16{}, y, ldy);
-  else write(BF16{}, y, ldy);
+  const auto write_as = [&](auto type, void* to, int64_t ld) __attribute__((always_inline)) {
+    if (int64_t(vt + 1) * MT * kTileVecs <= nvec) write(type, std::true_type{}, to, ld);
+    else write(type, std::false_type{}, to, ld);
+  };
+  if (splits > 1) write_as(F32{}, partial + split * nvec * q.nrows, q.nrows);
+  else if (ytype == SEEDQ_F32) write_as(F32{}, y, ldy);
+  else if (ytype == SEEDQ_F16) write_as(F16{}, y, ldy);
+  else write_as(BF16{}, y, ldy);
 }
 
 constexpr size_t kLdsBytes = 160 << 10;

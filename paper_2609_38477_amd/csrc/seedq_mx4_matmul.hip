@@ -120,7 +120,7 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 // one register that the products pick their byte of.
 constexpr int kBlocks = 8;   // of a stage
 
-template <int MT, int NT, int WM, int WN, bool SHORT>
+template <int MT, int NT, int WM, int WN, bool SHORT, bool FULL>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict__ y, int ytype,
             int64_t ldy, float* __restrict__ partial) {
@@ -140,16 +140,27 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
   const int lane = int(threadIdx.x & 63), n = lane & 31, kg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int wm = wave % WM, wn = wave / WM;
-  const int64_t i0 = int64_t(at) * kRowsA, j0 = int64_t(bt) * kRowsB;
-  // this lane's rows and blocks of the loads
-  const uint32_t* from[kLoads];
-  int block[kLoads];
+  // FULL: the last tiles are moved up until they are whole (what two make is the same), and
+  // so are the stages, so that no row and no block is past the last.
+  int64_t i0 = int64_t(at) * kRowsA, j0 = int64_t(bt) * kRowsB;
+  if constexpr (FULL) {
+    i0 = std::min(i0, a.nrows - kRowsA);
+    j0 = std::min(j0, b.nrows - kRowsB);
+  }
+  // This lane's rows and blocks of the loads: those of a load are a number of rows after the
+  // first one's that is the same for all lanes, and the blocks are the same.
+  static_assert(kWaves * 8 % 16 == 0, "the swizzle of a load's rows");
+  constexpr int kLoadsA = kRowsA / 8 / kWaves;
+  const int lrow = wave * 8 + (lane >> 3), lblock = (lane & 7) ^ ((lrow >> 1) & 7);
+  const uint32_t* from[FULL ? 1 : kLoads];
+  const uint32_t lane_bytes = uint32_t(lrow) * uint32_t(a.row_words * 4) + lblock * 16;   // FULL: fits
+  if constexpr (!FULL) {
 #pragma unroll
-  for (int k = 0; k < kLoads; ++k) {
-    const int r = (k * kWaves + wave) * 8 + (lane >> 3);
-    block[k] = (lane & 7) ^ ((r >> 1) & 7);
-    from[k] = r < kRowsA ? a.codes + std::min(i0 + r, a.nrows - 1) * a.row_words
-                         : b.codes + std::min(j0 + r - kRowsA, b.nrows - 1) * b.row_words;
+    for (int k = 0; k < kLoads; ++k) {
+      const int r = k * kWaves * 8 + lrow;
+      from[k] = r < kRowsA ? a.codes + std::min(i0 + r, a.nrows - 1) * a.row_words
+                           : b.codes + std::min(j0 + r - kRowsA, b.nrows - 1) * b.row_words;
+    }
   }
   // Exponents go to LDS sixteen blocks, two stages, at a time, a row a lane: a load of few
   // bytes of many rows costs as much as one of sixteen.
@@ -174,8 +185,15 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
   };
   // The loads of a stage one by one.
   const auto fetch = [&](int64_t stage, int buf, int i) __attribute__((always_inline)) {
-    to_lds16(from[i] + std::min(stage * kBlocks + block[i], nblocks - 1) * 4,
-             &lds[(buf * (kRowsA + kRowsB) + (i * kWaves + wave) * 8) * 8]);
+    const void* at;
+    if constexpr (FULL) {   // an address that is the same for all lanes, and the lane's offset
+      const uint32_t* all = i < kLoadsA ? a.codes + (i0 + i * kWaves * 8) * a.row_words
+                                        : b.codes + (j0 + (i - kLoadsA) * kWaves * 8) * b.row_words;
+      at = reinterpret_cast<const char*>(all + stage * (kBlocks * 4)) + lane_bytes;
+    } else {
+      at = from[i] + std::min(stage * kBlocks + lblock, nblocks - 1) * 4;
+    }
+    to_lds16(at, &lds[(buf * (kRowsA + kRowsB) + (i * kWaves + wave) * 8) * 8]);
   };
   floatx16 acc[MT][NT] = {};
 #pragma unroll
@@ -241,7 +259,7 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int64_t r = j0 + (wn * NT + j) * 32 + n;
-      if (r >= b.nrows) continue;
+      if (!FULL && r >= b.nrows) continue;
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t v0 = i0 + (wm * MT + i) * 32 + 4 * kg;
@@ -249,7 +267,9 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int v = 8 * (e >> 2) + (e & 3);
-          if (v0 + v < a.nrows) p[v * ld] = Y::narrow(acc[i][j][e]);
+          if (FULL || v0 + v < a.nrows) *p = Y::narrow(acc[i][j][e]);
+          p += (e & 3) == 3 ? 5 * ld : ld;
+          if (FULL) __builtin_amdgcn_sched_barrier(0);   // one address at a time
         }
       }
     }
@@ -325,9 +345,12 @@ hipError_t launch(const Mx4& a, const Mx4& b, void* d_y, int ytype, int64_t ldy,
       hipLaunchKernelGGL(kern, dim3(unsigned(units * p.a_tiles)), dim3(64 * waves), size_t(4) * p.tile * (128 + 16),
                          stream, a, b, p.a_tiles, p.b_tiles, p.splits, d_y, ytype, ldy, partial);
     };
-    if (b.nblocks < 16) go(tile_kernel<2, 2, 2, 2, true>, 4);
-    else if (p.tile == 256) go(tile_kernel<4, 2, 2, 4, false>, 8);
-    else go(tile_kernel<2, 2, 2, 2, false>, 4);
+    const bool full = a.nrows >= p.tile && b.nrows >= p.tile && b.nblocks % kBlocks == 0 &&
+                      b.row_words < int64_t(1) << 23;   // 64 rows are less than 2^32 bytes
+    if (b.nblocks < 16) go(tile_kernel<2, 2, 2, 2, true, false>, 4);
+    else if (p.tile == 256)
+      full ? go(tile_kernel<4, 2, 2, 4, false, true>, 8) : go(tile_kernel<4, 2, 2, 4, false, false>, 8);
+    else full ? go(tile_kernel<2, 2, 2, 2, false, true>, 4) : go(tile_kernel<2, 2, 2, 2, false, false>, 4);
   }
   if (p.splits > 1)
     hipLaunchKernelGGL(join_kernel, dim3(unsigned((b.nrows + 255) / 256), unsigned(a.nrows)), dim3(256), 0,
