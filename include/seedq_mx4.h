@@ -56,7 +56,8 @@ int seedq_mx4_dequantize(const uint32_t* d_codes, const uint8_t* d_scale, int64_
 
 /*
  * y_v = W_hat x_v for nvec >= 0 vectors, W_hat decoded on the fly and never stored.
- * The products are exact, the sums held in fp32, and y is rounded once.
+ * The products are exact (but for bits of fp32 vectors below 2^-133), the sums held in
+ * fp32, and y is rounded once.
  *   d_x: xtype [nvec][ncols], row stride ldx >= ncols elements.
  *   d_y: ytype [nvec][nrows], row stride ldy >= nrows elements; ytype is SEEDQ_F32
  *        or xtype. Not overlapping d_x.

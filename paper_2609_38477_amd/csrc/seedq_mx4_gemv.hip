@@ -764,6 +764,9 @@ hipError_t launch_gemm(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx,
 
 // The ways, and the vectors of one pass.
 constexpr int64_t kMaxVecs = 32768;
+// A batch's panels of longer rows than this would be many thousands, and the tiles' fragments
+// of few vectors, padded to 32, many times the vectors.
+constexpr int64_t kLongRow = int64_t(1) << 22;
 enum class Way { kFew, kBatch, kMany };
 Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   // The vector ALU takes two vectors, and up to four short ones where rows are few: us by it
@@ -778,7 +781,8 @@ Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   //   16 of fp16: 4096 x 4096 9.6 and 14.3, 8192 x 28672 42.1 and 63.6, 32000 x 4096 26.1 and 41.3
   //    8 of fp32: 4096 x 4096 8.6 and 15.1, 8192 x 28672 38.9 and 69.3, 32000 x 4096 24.1 and 43.0
   const int two = xtype == SEEDQ_F32 ? 8 : xtype == SEEDQ_F16 ? 16 : 32;
-  return nvec <= two && ncols > 15 * kMxBlock ? Way::kBatch : Way::kMany;   // a batch reads 16 exponents
+  if (nvec > two || ncols < 16 * kMxBlock) return Way::kMany;   // a batch reads 16 exponents
+  return ncols <= kLongRow ? Way::kBatch : Way::kFew;
 }
 int pieces_of(int xtype) { return xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1; }
 

@@ -304,7 +304,11 @@ struct Plan {
 };
 Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
   Plan p{};
-  if (na <= kFewRows && nblocks >= 16) {
+  // The kernel of few rows reads A again for every 16 rows of B: us by it and by tiles of 128
+  //   32 rows: 4096 x 4096 6.1 and 10.6, 14336 x 4096 21 and 18, 8192 x 28672 54 and 39
+  //   64 rows: 1001 x 2056 6.9 and 11.1, 2000 x 8192 16.8 and 12.4, 32000 x 4096 74 and 30
+  const bool few = na <= 16 || (na <= kFewRows && double(na) * nb * nblocks * kMxBlock < 1e9);
+  if (few && nblocks >= 16) {
     const int64_t steps = (nblocks + 4 * kStep - 1) / (4 * kStep);
     p.b_tiles = int((nb + 15) / 16);
     p.waves = int(std::min<int64_t>(kFewWaves, steps));

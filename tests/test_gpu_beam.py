@@ -235,3 +235,24 @@ def test_reorder_past_32_bits(sq, torch):  # noqa: F811
         assert torch.equal(got[j], state[p])
     sq.beam_reorder(state, parents, out=state)
     assert torch.equal(state, got)
+
+
+def test_more_sequences_than_a_launch(sq, torch):  # noqa: F811
+    batch, beams, vocab, top = 65536 + 9, 2, 24, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(batch * beams, vocab, generator=g, device="cuda")
+    scores = torch.randn(batch, beams, generator=g, device="cuda")
+    finished = torch.rand(batch, beams, generator=g, device="cuda") < 0.2
+    r = sq.beam_select(x, scores, top, finished=finished, pad_token=5)
+    for lo, hi in ((0, 40), (65530, batch)):
+        part = sq.BeamStep(r.score[lo:hi], r.parent[lo:hi], r.token[lo:hi])
+        check(part, x[lo * beams:hi * beams], scores[lo:hi], finished[lo:hi], 5, top)
+
+
+def test_many_offers_of_equal_total(sq, torch):  # noqa: F811
+    # every beam offers the same: the bounds of the join cut nothing away that counts
+    for beams, vocab, top in ((32, 70000, 32), (31, 40, 32), (16, 33000, 32), (5, 131072, 32), (32, 3, 17)):
+        x = torch.zeros(beams, vocab, device="cuda", dtype=torch.float16)
+        r = sq.beam_select(x, torch.zeros(1, beams, device="cuda"), top)
+        want = [(b, v) for b in range(beams) for v in range(min(vocab, top))][:top]
+        assert [(int(p), int(t)) for p, t in zip(r.parent[0], r.token[0])] == want
