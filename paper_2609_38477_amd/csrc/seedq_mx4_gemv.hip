@@ -77,6 +77,10 @@ __device__ __forceinline__ void split8(const typename X::raw* p, uint32x4 (&piec
 // on their way. In 16 bits two products a dot instruction, whose sum is fp32. Where rows are
 // few, `slices` waves share them, each with steps of its own. Order of the sums: the columns
 // of a lane, step after step, the lanes as a tree, the slices in order.
+// Memory bounds one vector (8192 x 28672 in bf16 24.7 us, 5.1 TB/s of codes and exponents;
+// 32000 x 4096 15.1, 4.6 TB/s), the vector ALU more: two vectors take 27.8 us, two of fp32,
+// an operation a product, 31.5. 4096 x 4096 takes 4.5, some 2 of them an empty launch. A
+// batch's kernel takes 30.5, 15.9 and 5.5 us for one vector: its loads touch 16 rows each.
 constexpr int kMaxWaves = 16;
 constexpr int kStepCols = 64 * kMxBlock;
 constexpr int kFewBytes = 128 << 10;
@@ -243,8 +247,12 @@ hipError_t launch_few(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx, 
     const size_t step_bytes = size_t(nv) * kStepCols * sizeof(raw);
     const int panel_steps = int(std::min<int64_t>(steps, kFewBytes / step_bytes));
     const int64_t batches = (q.nrows + rb - 1) / rb;
+    // Few rows of many columns are shared by several waves: 100 x 28672 4.9 us, one wave a row 7.5.
     const int slices = int(std::max<int64_t>(
         1, std::min<int64_t>({1024 / batches, panel_steps >= 4 ? panel_steps : 1, 8})));
+    // Large workgroups where the panel is large, small ones where rows are few: one bf16 vector with
+    // 16, 8 and 4 waves takes 25.5, 26.1 and 36.6 us at 8192 x 28672, 4.4, 4.5 and 4.7 at 4096 x
+    // 4096, three of fp32 7.2, 5.3 and 5.3 at 1001 x 2056.
     int waves = batches >= 4096 && panel_steps * step_bytes > (32 << 10) ? 16 : batches >= 2048 ? 8 : 4;
     waves = std::max(waves, slices) / slices * slices;
     const int slots = waves / slices;
@@ -255,7 +263,9 @@ hipError_t launch_few(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx, 
   };
   auto rows = [&](auto nv, int64_t v) {
     constexpr int NV = decltype(nv)::value;
-    const bool two = q.nrows >= 16384 || (NV > 1 && q.nrows >= 8192);
+    // Two rows a wave share what is read of x: 32000 x 4096 15.0 us (one row 17.0), and two
+    // vectors 18.3 (20.1); 14336 x 4096 and two 10.8 (9.7), 1001 x 2056 and three of fp32 6.2 (5.3).
+    const bool two = q.nrows >= 16384;
     two ? go(few_kernel<X, NV, 2>, NV, 2, v) : go(few_kernel<X, NV, 1>, NV, 1, v);
   };
   for (int64_t v = 0; v < nvec; v += 4) {
@@ -278,6 +288,11 @@ hipError_t launch_few(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx, 
 // before is multiplied with the pieces from LDS. Row i of a product lies in lanes 16 (i / 4) .., register i % 4,
 // so the pieces of a vector, which are neighbouring rows, meet in a lane. Slices meet in LDS
 // in order, panels in the join kernel.
+// Memory bounds it: 8192 x 28672 and 8 fp16 vectors take 26 us and the join 5 (4.8 TB/s of
+// codes and exponents while it runs), 16 of bf16 34.5 in all, 32 46; 4096 x 4096 and 8 7.5.
+// The cut matters as much as the code: with panels of 96 KB and 16 rows a wave throughout,
+// which left waves without rows, the first took 48. Exponents read a byte a lane and chunk
+// took 10 us more of 41.
 constexpr int kChunk = 128;
 constexpr int kDeep = 4;   // chunks of a step
 
@@ -464,6 +479,14 @@ join_kernel(const float* __restrict__ partial, int panels, int64_t nvec, int64_t
 // next stage's fragments and codes are on their way during the products. A lane's codes are
 // the 16 bytes of block l / 32 of a chunk of 64 columns of row l % 32; product t takes
 // everybody's word t.
+// 32000 x 4096 and 512 bf16 vectors take 119 to 128 us (1.05 to 1.13 PFLOP/s by box) after 6
+// for the fragments, of fp16 198, of fp32 318; a library product of the decoded 16-bit matrix
+// takes 97. Zero data takes 13 % less: the matrix core's power counts. Neither loads (all from
+// one stage: no change) nor the barrier bound it (one between two steps, with the next
+// stage's first fragments read before the last products: no change), but what is done for
+// every 128 vectors again, conversions and loads of codes, and 10 us of results that all
+// workgroups write at the end. Fragments read right before their use took 142, the next
+// stage's loads issued together 137; 64 vectors a tile take 164, one tile of rows a wave 133.
 constexpr int kFrags = 4;       // of 64 lanes x 16 bytes: a chunk of 64 columns, 32 vectors, each piece
 constexpr int kTileVecs = 32;
 
@@ -717,13 +740,20 @@ GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
   const int64_t tiles = (nvec + kTileVecs - 1) / kTileVecs;
   const int most = pieces == 3 ? 3 : 4;
   p.mt = 1;
-  for (int m = 2; m <= most; ++m)   // the fewest tiles in all, then the widest
+  // The fewest tiles of vectors in all, then the widest: a wider one decodes less often (32000 x
+  // 4096 and 512 vectors in tiles of 128 123 us, of 64 164; 4096 x 4096 and 128 27 and 22).
+  for (int m = 2; m <= most; ++m)
     if ((tiles + m - 1) / m * m <= (tiles + p.mt - 1) / p.mt * p.mt) p.mt = m;
   p.vec_tiles = int((tiles + p.mt - 1) / p.mt);
+  // 64 rows a wave where that leaves as many tiles as the chip holds workgroups: 32000 x 4096 and
+  // 512 vectors 123 us (32 rows 133), 14336 x 4096 and 512 84 (66), 4096 x 4096 and 512 43 (35).
   p.rt = (nrows + 255) / 256 * p.vec_tiles >= 400 ? 2 : 1;
   p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
   p.chunks = (ncols + 127) / 128 * 2;   // whole stages
   const int64_t all = int64_t(p.vec_tiles) * p.row_tiles;
+  // Up to two workgroups a CU, of four stages at least: 4096 x 4096 and 300 vectors up to 512
+  // workgroups 30.1 us, 256 39.5, 1024 33.2; 4096 x 4096 and 64 four stages 17.5, two 22.4,
+  // eight 18.5.
   p.splits = int(std::max<int64_t>(1, std::min<int64_t>({512 / all, p.chunks / 8, 32})));
   p.frags = align256(size_t(p.vec_tiles) * p.mt * p.chunks * pieces * kFrags * 1024);
   p.total = p.frags;

@@ -26,7 +26,9 @@ __device__ __forceinline__ intx8 fp4_operand(uint32x4 c) {
 // 16 AT rows of A against 16 rows of B a workgroup. The waves divide the columns in steps of
 // 512, whose codes and exponents a lane reads straight into registers, the next step's
 // during the products; their sums meet in LDS in order. A's rows are the same for all
-// workgroups and come from the caches.
+// workgroups and come from the caches. 4 x 4096 x 4096 take 4.2 us, some 2 of them an empty
+// launch, 4 x 8192 x 28672 29 (4.3 TB/s), bound by memory; 16 x 8192 x 28672 37, bound by the
+// loads of A.
 constexpr int kStep = 4;        // products of a step
 constexpr int kFewWaves = 8;
 
@@ -118,6 +120,12 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 // place j ^ (r / 2 % 8) of the row's eight, so that the 16 bytes that neighbouring lanes
 // read, of neighbouring rows, spread over all banks. A lane's four exponents of a stage are
 // one register that the products pick their byte of.
+// 2048 x 32000 x 4096 take 175 to 187 us by box (2.9 to 3.1 PFLOP/s), 2048 x 8192 x 28672 293
+// (3.3), 512 x 14336 x 4096 24. Products alone, without loads, reach 6.7 PFLOP/s on random data
+// and 5.2 with as many reads of LDS: power holds them, zeros take a quarter less. What else
+// bounds it are the waits at a stage's start. Exponents read by eight bytes of a row a lane took
+// 210 us, operands read right before their use 265. Tried and dropped: two workgroups a CU
+// with stages of 128 columns (216), the barrier before a stage's last step (registers spill).
 constexpr int kBlocks = 8;   // of a stage
 
 template <int MT, int NT, int WM, int WN, bool SHORT, bool FULL>
@@ -315,6 +323,9 @@ Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
     p.splits = int(std::max<int64_t>(1, std::min<int64_t>({256 / p.b_tiles, steps / (2 * p.waves), 16})));
   } else {
     const int64_t stages = (nblocks + kBlocks - 1) / kBlocks;
+    // Tiles of 256 where there is one for each CU, of 128 else: 2048 x 32000 x 4096 175 us (128: 234),
+    // 512 x 14336 x 4096 58 (24), 2048 x 4096 x 4096 69 (27). Up to two workgroups a CU, of four
+    // stages at least: 128 x 4096 x 4096 15.1 us, of two stages 19.1, of one 22.9.
     const auto tiles = [&](int64_t t) { return ((na + t - 1) / t) * ((nb + t - 1) / t); };
     p.tile = na > 128 && tiles(256) >= 256 && nblocks >= 16 ? 256 : 128;
     p.a_tiles = int((na + p.tile - 1) / p.tile), p.b_tiles = int((nb + p.tile - 1) / p.tile);
