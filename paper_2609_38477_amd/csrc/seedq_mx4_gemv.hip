@@ -663,13 +663,14 @@ struct BatchPlan {
 };
 // The cut that the following model finds fastest, in us. A wave goes through its chunks at
 // its share of the memory's rate, 1 KB RT in 0.84 RT with all waves at work, but no faster
-// than its loads in flight allow; a workgroup lays out its panel; panels cost a second
+// than its loads in flight, its CU's part of that rate and the CU's LDS allow, and starts and
+// ends the sums of each of its rows; a workgroup lays out its panel; panels cost a second
 // launch and its traffic.
 BatchPlan batch_plan(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   const int pieces = xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1;
   const int each = xtype == SEEDQ_F32 ? 4 : xtype == SEEDQ_F16 ? 8 : 16;
   BatchPlan best{};
-  const int xt = nvec <= each ? 1 : 2, rt = xt;
+  const int xt = nvec <= each ? 1 : nvec <= 2 * each ? 2 : 4, rt = xt == 2 ? 2 : 1;
   const int most = xt == 1 ? 16 : 8;
   const int64_t chunk_bytes = int64_t(pieces) * nvec * 256;
   const int chunks = int((ncols + kChunk - 1) / kChunk);
@@ -692,7 +693,7 @@ BatchPlan batch_plan(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
     p.grid = unsigned(std::min(units, per_panel));
     const double rounds = double((units + p.grid - 1) / p.grid);
     const double busy = double(p.grid) * p.panels * p.waves / (kWorkgroups * 16.0);
-    const double chunk = std::max({0.3, 0.84 * rt * busy, 0.7 * rt * p.waves / 16});
+    const double chunk = std::max({0.3, 0.84 * rt * busy, 0.7 * rt * p.waves / 16, 0.015 * xt * p.waves});
     const double us = rounds * (((steps + p.cut.slices - 1) / p.cut.slices) * kDeep * chunk +
                                 (p.cut.slices > 1 ? 0.8 : 0.4)) +
                       p.cut.panel_chunks * chunk_bytes / 6e4 +
@@ -722,7 +723,8 @@ hipError_t launch_batch(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx
                        partial);
   };
   if (p.xt == 1) go(batch_kernel<X, 1, 1>);
-  else go(batch_kernel<X, 2, 2>);
+  else if (p.xt == 2) go(batch_kernel<X, 2, 2>);
+  else if constexpr (!std::is_same_v<X, BF16>) go(batch_kernel<X, 4, 1>);   // see way
   if (p.panels > 1)
     hipLaunchKernelGGL(join_kernel, dim3(unsigned((q.nrows + 255) / 256), unsigned(nvec)), dim3(256), 0,
                        stream, partial, p.panels, nvec, q.nrows, d_y, ytype, ldy);
@@ -806,12 +808,13 @@ Way way(int64_t nrows, int64_t ncols, int64_t nvec, int xtype) {
   //   4 of fp32: 4096 x 4096 8.8 and 7.9, 2000 x 8192 18.4 and 8.4, 8192 x 28672 45.8 and 34.3
   const int size = xtype == SEEDQ_F32 ? 4 : 2;
   if (nvec <= 2 || (nvec <= 4 && nrows <= 8192 && nvec * ncols * size <= 48 << 10)) return Way::kFew;
-  // A batch takes two tiles: us by it and by the tiles for many
+  // A batch takes two tiles of pieces, and four of fp16 and fp32: us by it and by the tiles for many
   //   32 of bf16: 4096 x 4096 11.4 and 13.6, 8192 x 28672 45.9 and 53.3, 32000 x 4096 30.5 and 35.5
-  //   16 of fp16: 4096 x 4096 9.6 and 14.3, 8192 x 28672 42.1 and 63.6, 32000 x 4096 26.1 and 41.3
-  //    8 of fp32: 4096 x 4096 8.6 and 15.1, 8192 x 28672 38.9 and 69.3, 32000 x 4096 24.1 and 43.0
-  const int two = xtype == SEEDQ_F32 ? 8 : xtype == SEEDQ_F16 ? 16 : 32;
-  if (nvec > two || ncols < 16 * kMxBlock) return Way::kMany;   // a batch reads 16 exponents
+  //   64 of bf16: 4096 x 4096 22.1 and 16.9, 8192 x 28672 109 and 62
+  //   32 of fp16: 4096 x 4096 13.4 and 15.8, 8192 x 28672 67.6 and 65.8, 32000 x 4096 40.7 and 45.7
+  //   16 of fp32: 4096 x 4096 10.7 and 16.0, 8192 x 28672 51.6 and 72.1, 32000 x 4096 30.7 and 46.1
+  const int most = xtype == SEEDQ_F32 ? 16 : 32;
+  if (nvec > most || ncols < 16 * kMxBlock) return Way::kMany;   // a batch reads 16 exponents
   return ncols <= kLongRow ? Way::kBatch : Way::kFew;
 }
 int pieces_of(int xtype) { return xtype == SEEDQ_F32 ? 3 : xtype == SEEDQ_F16 ? 2 : 1; }
