@@ -183,8 +183,8 @@ def beam_reorder(states, parents, out=None, stream=None):
     states: a tensor or a list of tensors of any type on the GPU, [batch * beams, ...]
     each with the same number of rows; a row may be a part of a larger cache (a view).
     parents: int64 [batch, out_beams]. ``out``: tensors of the results' shapes and the
-    states' types, or the states themselves, whose rows are then moved in place (those
-    that are their own parents stay untouched). Returns a tensor or a list like states."""
+    states' types that overlap nothing else of the call, or the states themselves, whose
+    rows are then moved in place (those that are their own parents stay untouched). Returns a tensor or a list like states."""
     import torch
     single = isinstance(states, torch.Tensor)
     states = [states] if single else list(states)
@@ -236,6 +236,11 @@ def beam_reorder(states, parents, out=None, stream=None):
                 keep.append(s)
                 at, moved = s.data_ptr(), _moved(shape, s.stride(), to, s.element_size())
             fields += (at, to_at, *moved)
+        if out is not None:
+            sources, targets = set(fields[::8]), fields[1::8]
+            if len(set(targets)) != len(targets) or any(
+                    to != at and to in sources for at, to in zip(fields[::8], targets)):
+                raise ValueError("out: tensors that are no other result's and no other state wanted")
         if fields:
             array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
             _check(lib().seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,

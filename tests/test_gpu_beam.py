@@ -200,6 +200,28 @@ def test_reorder_in_place(sq, torch, batch, beams):  # noqa: F811
         assert torch.equal(cache[:, :, 41:], before[:, :, 41:])
 
 
+def test_reorder_refuses(sq, torch):  # noqa: F811
+    a, b = torch.randn(4, 6).cuda(), torch.randn(4, 6).cuda()
+    p = torch.tensor([[1, 0], [0, 0]]).cuda()
+    wide = torch.randn(4, 12).cuda()
+    before = [a.clone(), b.clone()]
+    for states, out in (([a, a], [a, a]), ([a, b], [b, a]), ([a, b], [wide[:, :6], wide[:, :6]]), ([a], [a[:2]]),
+                        ([a], [a.double()]), ([a], [a.cpu()]), ([a], []), ([a, b[:2]], None), ([a.cpu()], None),
+                        ([a[:3]], None), ([a], [torch.empty_like(a)[:1].expand(4, 6)])):
+        with pytest.raises((ValueError, sq.SeedqError)):
+            sq.beam_reorder(states, p, out=out)
+    with pytest.raises(ValueError):
+        sq.beam_reorder(a, torch.zeros(4, 1, dtype=torch.int64).cuda(), out=a.t())
+    with pytest.raises(ValueError):
+        sq.beam_reorder(torch.randn(4, 6).cuda(), torch.zeros(2, 3, dtype=torch.int64).cuda(), out=a)
+    with pytest.raises(ValueError):
+        sq.beam_reorder(a, p.int())
+    assert torch.equal(a, before[0]) and torch.equal(b, before[1])
+    across = torch.zeros(6, 4).cuda().t()              # rows between each other's pieces
+    sq.beam_reorder(a, p, out=across)
+    assert torch.equal(across, sq.beam_reorder(a, p))
+
+
 def test_reorder_of_parents_that_are_none(sq, torch):  # noqa: F811
     state = torch.randn(8, 70, device="cuda")
     parents = torch.tensor([[-1, 0, 4, 3], [1 << 40, -(1 << 62), 2, 2]]).cuda()

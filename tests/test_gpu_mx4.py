@@ -343,3 +343,24 @@ def test_in_a_graph(sq, torch):  # noqa: F811
         torch.cuda.synchronize()
         for a, b in zip(outs, step()):
             assert torch.equal(a, b)
+
+
+def test_helpers_refuse(sq, torch):  # noqa: F811
+    q, _ = random_mx4(sq, torch, np.random.default_rng(1), 9, 72)
+    x = torch.zeros(2, 72, device="cuda")
+    for bad in (lambda: sq.mx4_gemv(q, x[:, :64]), lambda: sq.mx4_gemv(q, x.cpu()),
+                lambda: sq.mx4_gemv(sq.Mx4Weights(q.codes[:, :8], q.scale, 9, 72), x),
+                lambda: sq.mx4_gemv(sq.Mx4Weights(q.codes, q.scale[:8], 9, 72), x),
+                lambda: sq.mx4_gemv(sq.Mx4Weights(q.codes, q.scale.int(), 9, 72), x),
+                lambda: sq.mx4_gemv(sq.Mx4Weights(q.codes, q.scale, 9, 104), torch.zeros(2, 104, device="cuda")),
+                lambda: sq.mx4_matmul(q, sq.Mx4Weights(q.codes[:, :8], q.scale[:, :2], 9, 64)),
+                lambda: sq.mx4_dequantize(sq.Mx4Weights(q.codes.cpu(), q.scale, 9, 72))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(sq.SeedqError):
+        sq.mx4_quantize(torch.zeros(3, 12, device="cuda"))          # columns not in eights
+    with pytest.raises(sq.SeedqError):                              # codes that are not at 16 bytes
+        flat = torch.zeros(9 * 12 + 1, dtype=torch.int32, device="cuda")
+        sq.mx4_gemv(sq.Mx4Weights(flat[1:].view(9, 12), q.scale, 9, 72), x)
+    with pytest.raises(TypeError):
+        sq.mx4_gemv(q, x.double())
