@@ -16,13 +16,14 @@ from dataclasses import dataclass
 
 from . import _check, _ptr, _stream
 from . import lib as _base_lib
-from .ops import _handle, _logits, _on, _rows, _same
+from .ops import _logits, _on, _rows, _same
 
 SEEDQ_MAX_BEAMS = 32
 SEEDQ_MAX_BEAM_TOP = 32
 SEEDQ_MAX_BEAM_STATES = 4096
 
 _lib = None
+torch = _handle = _current_device = None   # from the first call on
 
 
 class BeamState(ctypes.Structure):
@@ -32,8 +33,10 @@ class BeamState(ctypes.Structure):
 
 
 def lib() -> ctypes.CDLL:
-    global _lib
+    global _lib, torch, _handle, _current_device
     if _lib is None:
+        import torch
+        _handle, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         L = _base_lib()
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         L.seedq_beam_select_workspace_bytes.restype = sz
@@ -90,34 +93,39 @@ def beam_select(logits, scores, top: int, finished=None, pad_token: int = 0, str
     scores fp32 [batch, beams] (the log probabilities so far, -inf for a dead beam).
     A beam that is ``finished`` (bool or uint8 [batch, beams]) is continued by pad_token
     alone, at its own score."""
-    import torch
+    L = _lib or lib()
     t, device = _logits(logits, "logits")
-    if scores.dim() != 2 or scores.shape[1] < 1 or scores.shape[1] > SEEDQ_MAX_BEAMS:
+    nrows, vocab = logits.shape
+    if scores.dim() != 2 or not 1 <= scores.shape[1] <= SEEDQ_MAX_BEAMS:
         raise ValueError(f"scores: [batch, 1 to {SEEDQ_MAX_BEAMS} beams] wanted, not {tuple(scores.shape)}")
     batch, beams = scores.shape
-    nrows, vocab = logits.shape
     if nrows != batch * beams:
         raise ValueError(f"logits: {batch * beams} rows wanted, not {nrows}")
     if not 1 <= top <= SEEDQ_MAX_BEAM_TOP:
         raise ValueError(f"top: 1 to {SEEDQ_MAX_BEAM_TOP} wanted, not {top}")
     _same(scores, device, (batch, beams), torch.float32, "scores")
     if finished is not None:
-        if finished.dtype != torch.bool:
-            _same(finished, device, (batch, beams), torch.uint8, "finished")
-        else:
-            _same(finished, device, (batch, beams), torch.bool, "finished")
+        _same(finished, device, (batch, beams), torch.bool if finished.dtype == torch.bool else torch.uint8,
+              "finished")
         if pad_token < 0:
             raise ValueError(f"pad_token: not negative wanted, not {pad_token}")
+    if stream is None:
+        return _select(L, logits, t, device, scores, batch, beams, vocab, top, finished, pad_token)
     with _on(stream):
-        x, ld = _rows(logits)
-        score = x.new_empty((batch, top), dtype=torch.float32)
-        parent, token = x.new_empty((2, batch, top), dtype=torch.int64).unbind(0)
-        nws = _select_workspace(batch, beams, vocab, top)
-        ws = x.new_empty(nws, dtype=torch.uint8) if nws else None
-        _check(lib().seedq_beam_select(x.data_ptr(), t, ld, batch, beams, vocab, scores.data_ptr(),
-                                       _ptr(finished), pad_token, top, score.data_ptr(),
-                                       parent.data_ptr(), token.data_ptr(), _ptr(ws), nws,
-                                       _handle(device)), "seedq_beam_select")
+        return _select(L, logits, t, device, scores, batch, beams, vocab, top, finished, pad_token)
+
+
+def _select(L, logits, t, device, scores, batch, beams, vocab, top, finished, pad_token):
+    x, ld = _rows(logits)
+    score = scores.new_empty((batch, top))
+    parent = x.new_empty((batch, top), dtype=torch.int64)
+    token = torch.empty_like(parent)
+    nws = _select_workspace(batch, beams, vocab, top)
+    ws = x.new_empty(nws, dtype=torch.uint8)
+    _check(L.seedq_beam_select(x.data_ptr(), t, ld, batch, beams, vocab, scores.data_ptr(),
+                               None if finished is None else finished.data_ptr(), pad_token, top,
+                               score.data_ptr(), parent.data_ptr(), token.data_ptr(), ws.data_ptr(), nws,
+                               _handle(device)), "seedq_beam_select")
     return BeamStep(score, parent, token)
 
 
@@ -184,8 +192,9 @@ def beam_reorder(states, parents, out=None, stream=None):
     each with the same number of rows; a row may be a part of a larger cache (a view).
     parents: int64 [batch, out_beams]. ``out``: tensors of the results' shapes and the
     states' types that overlap nothing else of the call, or the states themselves, whose
-    rows are then moved in place (those that are their own parents stay untouched). Returns a tensor or a list like states."""
-    import torch
+    rows are then moved in place (those that are their own parents stay untouched). Returns
+    a tensor or a list like states."""
+    L = _lib or lib()
     single = isinstance(states, torch.Tensor)
     states = [states] if single else list(states)
     if parents.dim() != 2 or not 1 <= parents.shape[1] <= SEEDQ_MAX_BEAMS:
@@ -194,7 +203,7 @@ def beam_reorder(states, parents, out=None, stream=None):
         raise ValueError(f"states: {SEEDQ_MAX_BEAM_STATES} at the most, not {len(states)}")
     batch, out_beams = parents.shape
     device = parents.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != _current_device():
         raise ValueError(f"parents: on {parents.device}, not on the current GPU")
     _same(parents, device, (batch, out_beams), torch.int64, "parents")
     if out is not None:
@@ -206,44 +215,53 @@ def beam_reorder(states, parents, out=None, stream=None):
     if states and (rows != batch * beams or not 1 <= beams <= SEEDQ_MAX_BEAMS):
         raise ValueError(f"states: rows of {batch} sequences of 1 to {SEEDQ_MAX_BEAMS} beams wanted, "
                          f"not {rows}")
-    out_rows = batch * out_beams
-    with _on(stream):
-        results, fields, keep = [], [], []
-        for k, s in enumerate(states):
-            shape = s.shape
-            if not shape or shape[0] != rows or s.get_device() != device:
-                raise ValueError(f"states: tensors of {rows} rows on GPU {device} wanted, not "
-                                 f"{tuple(shape)} on {s.device}")
-            if out is None:
-                o, to = s.new_empty((out_rows, *shape[1:])), None
-            else:
-                o = out[k]
-                if o.dtype != s.dtype or o.shape != (out_rows, *shape[1:]) or o.get_device() != device:
-                    raise ValueError(f"out: {s.dtype} of shape {(out_rows, *shape[1:])} on GPU {device} "
-                                     f"wanted, not {o.dtype} {tuple(o.shape)} on {o.device}")
-                to = o.stride()
-                if _pieces(o.shape, to, 1) is None:
-                    raise ValueError("out: rows that are pieces at one stride wanted")
-            results.append(o)
-            at, to_at = s.data_ptr(), o.data_ptr()
-            if not at or not to_at:   # no elements
-                continue
-            if at == to_at and (s.stride() != to or out_beams != beams):
-                raise ValueError("out: in place, the states' own layout and number of beams wanted")
-            moved = _moved(shape, s.stride(), to, s.element_size())
-            if moved is None:
-                s = s.contiguous()
-                keep.append(s)
-                at, moved = s.data_ptr(), _moved(shape, s.stride(), to, s.element_size())
-            fields += (at, to_at, *moved)
-        if out is not None:
-            sources, targets = set(fields[::8]), fields[1::8]
-            if len(set(targets)) != len(targets) or any(
-                    to != at and to in sources for at, to in zip(fields[::8], targets)):
-                raise ValueError("out: tensors that are no other result's and no other state wanted")
-        if fields:
-            array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
-            _check(lib().seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,
-                                            out_beams, _handle(device)), "seedq_beam_reorder")
+    args = (L, states, parents, out, rows, batch, beams, out_beams, device)
+    if stream is None:
+        results = _reorder(*args)
+    else:
+        with _on(stream):
+            results = _reorder(*args)
     return results[0] if single else results
 
+
+def _reorder(L, states, parents, out, rows, batch, beams, out_beams, device):
+    out_rows, same = batch * out_beams, beams == out_beams
+    new, dense = torch.empty_like, torch.contiguous_format
+    results, fields, keep = [], [], []
+    for k, s in enumerate(states):
+        shape = s.shape
+        if not shape or shape[0] != rows or s.get_device() != device:
+            raise ValueError(f"states: tensors of {rows} rows on GPU {device} wanted, not "
+                             f"{tuple(shape)} on {s.device}")
+        if out is None:
+            o, to = (new(s, memory_format=dense) if same else s.new_empty((out_rows, *shape[1:]))), None
+        else:
+            o = out[k]
+            if o.dtype != s.dtype or o.shape != (out_rows, *shape[1:]) or o.get_device() != device:
+                raise ValueError(f"out: {s.dtype} of shape {(out_rows, *shape[1:])} on GPU {device} "
+                                 f"wanted, not {o.dtype} {tuple(o.shape)} on {o.device}")
+            to = o.stride()
+            if _pieces(o.shape, to, 1) is None:
+                raise ValueError("out: rows that are pieces at one stride wanted")
+        results.append(o)
+        at, to_at = s.data_ptr(), o.data_ptr()
+        if not at or not to_at:   # no elements
+            continue
+        if at == to_at and (s.stride() != to or out_beams != beams):
+            raise ValueError("out: in place, the states' own layout and number of beams wanted")
+        moved = _moved(shape, s.stride(), to, s.element_size())
+        if moved is None:
+            s = s.contiguous()
+            keep.append(s)
+            at, moved = s.data_ptr(), _moved(shape, s.stride(), to, s.element_size())
+        fields += (at, to_at, *moved)
+    if out is not None:
+        sources, targets = set(fields[::8]), fields[1::8]
+        if len(set(targets)) != len(targets) or any(
+                to != at and to in sources for at, to in zip(fields[::8], targets)):
+            raise ValueError("out: tensors that are no other result's and no other state wanted")
+    if fields:
+        array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
+        _check(L.seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,
+                                    out_beams, _handle(device)), "seedq_beam_reorder")
+    return results
