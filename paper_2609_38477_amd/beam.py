@@ -233,10 +233,15 @@ def _reorder(L, states, parents, out, rows, batch, beams, out_beams, device):
         if not shape or shape[0] != rows or s.get_device() != device:
             raise ValueError(f"states: tensors of {rows} rows on GPU {device} wanted, not "
                              f"{tuple(shape)} on {s.device}")
+        if s.is_conj() or s.is_neg():   # memory does not hold its values
+            s = s.resolve_conj().resolve_neg()
+            keep.append(s)
         if out is None:
             o, to = (new(s, memory_format=dense) if same else s.new_empty((out_rows, *shape[1:]))), None
         else:
             o = out[k]
+            if o.is_conj() or o.is_neg():
+                raise ValueError("out: tensors whose memory holds their values wanted")
             if o.dtype != s.dtype or o.shape != (out_rows, *shape[1:]) or o.get_device() != device:
                 raise ValueError(f"out: {s.dtype} of shape {(out_rows, *shape[1:])} on GPU {device} "
                                  f"wanted, not {o.dtype} {tuple(o.shape)} on {o.device}")

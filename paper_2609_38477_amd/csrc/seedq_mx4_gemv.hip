@@ -80,7 +80,7 @@ __device__ __forceinline__ void split8(const typename X::raw* p, uint32x4 (&piec
 // Memory bounds one vector (8192 x 28672 in bf16 24.7 us, 5.1 TB/s of codes and exponents;
 // 32000 x 4096 15.1, 4.6 TB/s), the vector ALU more: two vectors take 27.8 us, two of fp32,
 // an operation a product, 31.5. 4096 x 4096 takes 4.5, some 2 of them an empty launch. A
-// batch's kernel takes 30.5, 15.9 and 5.5 us for one vector: its loads touch 16 rows each.
+// batch's kernel takes 30.5, 16.3 and 5.5 us for one vector: its loads touch 16 rows each.
 constexpr int kMaxWaves = 16;
 constexpr int kStepCols = 64 * kMxBlock;
 constexpr int kFewBytes = 128 << 10;

@@ -229,6 +229,19 @@ def test_reorder_of_parents_that_are_none(sq, torch):  # noqa: F811
     assert np.array_equal(got.cpu().numpy(), obeam.reorder(state.cpu().numpy(), parents.cpu().numpy()))
 
 
+def test_reorder_of_complex_states(sq, torch):  # noqa: F811
+    state = torch.randn(6, 5, dtype=torch.complex64, device="cuda")
+    parents = torch.tensor([[2, 0, 2], [1, 1, 0]]).cuda()
+    at = torch.tensor([2, 0, 2, 4, 4, 3]).cuda()
+    # conjugates and their imaginary parts are marks on the same memory
+    states = [state, state.conj(), state.conj().imag]
+    for s, o in zip(states, sq.beam_reorder(states, parents)):
+        assert torch.equal(o, s.resolve_conj()[at])
+    for s in states[1:]:
+        with pytest.raises(ValueError):
+            sq.beam_reorder(s, parents, out=s)
+
+
 def test_reorder_of_many_states_and_sequences(sq, torch):  # noqa: F811
     g = torch.Generator().manual_seed(5)
     parents = torch.randint(3, (2, 3), generator=g).cuda()
