@@ -456,19 +456,6 @@ batch_kernel(Mx4 q, int nvec, const typename X::raw* __restrict__ x, int64_t ldx
   }
 }
 
-// The panels' sums added in order.
-__global__ void __launch_bounds__(256)
-join_kernel(const float* __restrict__ partial, int panels, int64_t nvec, int64_t nrows,
-            void* __restrict__ y, int ytype, int64_t ldy) {
-  const int64_t v = blockIdx.y;
-  const int64_t r = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (r >= nrows) return;
-  float sum = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < panels; ++s) sum += partial[(s * nvec + v) * nrows + r];
-  store_y(y, ytype, v * ldy + r, sum);
-}
-
 // ---------------------------------------------------------------- many vectors
 
 // A workgroup of four waves makes 32 MT vectors x 128 RT rows, a wave 32 RT of the rows, in
@@ -726,8 +713,7 @@ hipError_t launch_batch(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx
   else if (p.xt == 2) go(batch_kernel<X, 2, 2>);
   else if constexpr (!std::is_same_v<X, BF16>) go(batch_kernel<X, 4, 1>);   // see way
   if (p.panels > 1)
-    hipLaunchKernelGGL(join_kernel, dim3(unsigned((q.nrows + 255) / 256), unsigned(nvec)), dim3(256), 0,
-                       stream, partial, p.panels, nvec, q.nrows, d_y, ytype, ldy);
+    launch_join(partial, p.panels, nvec, q.nrows, d_y, ytype, ldy, stream);
   return hipGetLastError();
 }
 
@@ -789,8 +775,7 @@ hipError_t launch_gemm(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx,
   else if (p.mt == 3) with(std::integral_constant<int, 3>{});
   else if constexpr (P < 3) with(std::integral_constant<int, 4>{});
   if (p.splits > 1)
-    hipLaunchKernelGGL(join_kernel, dim3(unsigned((q.nrows + 255) / 256), unsigned(nvec)), dim3(256), 0,
-                       stream, partial, p.splits, nvec, q.nrows, d_y, ytype, ldy);
+    launch_join(partial, p.splits, nvec, q.nrows, d_y, ytype, ldy, stream);
   return hipGetLastError();
 }
 

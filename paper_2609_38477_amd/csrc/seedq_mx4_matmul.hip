@@ -288,19 +288,6 @@ tile_kernel(Mx4 a, Mx4 b, int a_tiles, int b_tiles, int splits, void* __restrict
   else write(BF16{}, y, ldy);
 }
 
-// The splits of the columns added in order.
-__global__ void __launch_bounds__(256)
-join_kernel(const float* __restrict__ partial, int splits, int64_t na, int64_t nb, void* __restrict__ y,
-            int ytype, int64_t ldy) {
-  const int64_t v = blockIdx.y;
-  const int64_t r = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (r >= nb) return;
-  float sum = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) sum += partial[(s * na + v) * nb + r];
-  store_y(y, ytype, v * ldy + r, sum);
-}
-
 // Rows of A of one pass: the grids stay small, and so does the workspace.
 constexpr int64_t kMaxVecs = 32768;
 constexpr int kFewRows = 64;
@@ -323,14 +310,29 @@ Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
     p.splits = int(std::max<int64_t>(1, std::min<int64_t>({256 / p.b_tiles, steps / (2 * p.waves), 16})));
   } else {
     const int64_t stages = (nblocks + kBlocks - 1) / kBlocks;
-    // Tiles of 256 where there is one for each CU, of 128 else: 2048 x 32000 x 4096 175 us (128: 234),
-    // 512 x 14336 x 4096 58 (24), 2048 x 4096 x 4096 69 (27). Up to two workgroups a CU, of four
-    // stages at least: 128 x 4096 x 4096 15.1 us, of two stages 19.1, of one 22.9.
+    // Times in rounds of 256 tiles of 256, one a CU, of which a last one costs less where it is not
+    // whole; 256 tiles of 128, which run two a CU, cost 0.3 of that. us by tiles of 256 and of 128
+    //   2048 x 32000 x 4096: 171 and 200, 1024 x 32000 x 4096 80 and 94, 640 x 32000 x 4096 69 and 61
+    //   4096 x 4096 x 4096: 43 and 52, 4352 x 4096 x 4096 68 and 62, 2048 x 4096 x 4096 26 by 128
+    //   1024 x 14336 x 4096: 39 and 45, 1152 x 14336 x 4096 67 and 47, 2048 x 8192 x 28672 253 and 332
     const auto tiles = [&](int64_t t) { return ((na + t - 1) / t) * ((nb + t - 1) / t); };
-    p.tile = na > 128 && tiles(256) >= 256 && nblocks >= 16 ? 256 : 128;
+    const int64_t large = tiles(256), small = tiles(128), last = large % 256;
+    const double by_large = double(large / 256) + (last ? 0.62 + 0.38 * double(last) / 256 : 0.0);
+    p.tile = nblocks >= 16 && by_large <= 0.3 * double((small + 255) / 256) ? 256 : 128;
     p.a_tiles = int((na + p.tile - 1) / p.tile), p.b_tiles = int((nb + p.tile - 1) / p.tile);
-    p.splits = int(std::max<int64_t>(
-        1, std::min<int64_t>({512 / (int64_t(p.a_tiles) * p.b_tiles), stages / 4, 16})));
+    // Splits of the columns, as many as two workgroups a CU: the fastest by 0.95 us a stage of
+    // one workgroup a CU, 1.2 of two, and 3 for the join and 0.6 for every MB of its sums. us
+    //   65 x 4096 x 4096: none 15.3, two 13.1, four 11.7, eight 13.4; 512 x 4096 x 4096 13.7, 21.4, 22.4
+    //   65 x 8192 x 28672: 94, 54, 41, 35; 256 x 8192 x 28672 115, 69, 61, 72
+    p.splits = 1;
+    double least = 0.0;
+    for (int64_t n = 1; p.tile == 128 && n <= std::min<int64_t>(stages, 16) && (n == 1 || small * n <= 512); ++n) {
+      const double us = double((stages + n - 1) / n) * (small * n <= 256 ? 0.95 : 1.2) +
+                        (n > 1 ? 3.0 + 0.6e-6 * double(n * na * nb) * sizeof(float) : 0.0);
+      if (n > 1 && us >= least) continue;
+      least = us;
+      p.splits = int(n);
+    }
   }
   p.partial = p.splits > 1 ? align256(size_t(p.splits) * na * nb * sizeof(float)) : 0;
   return p;
@@ -368,8 +370,7 @@ hipError_t launch(const Mx4& a, const Mx4& b, void* d_y, int ytype, int64_t ldy,
     else full ? go(tile_kernel<2, 2, 2, 2, false, true>, 4) : go(tile_kernel<2, 2, 2, 2, false, false>, 4);
   }
   if (p.splits > 1)
-    hipLaunchKernelGGL(join_kernel, dim3(unsigned((b.nrows + 255) / 256), unsigned(a.nrows)), dim3(256), 0,
-                       stream, partial, p.splits, a.nrows, b.nrows, d_y, ytype, ldy);
+    launch_join(partial, p.splits, a.nrows, b.nrows, d_y, ytype, ldy, stream);
   return hipGetLastError();
 }
 
