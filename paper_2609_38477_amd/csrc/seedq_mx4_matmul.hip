@@ -299,10 +299,15 @@ struct Plan {
 };
 Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
   Plan p{};
-  // The kernel of few rows reads A again for every 16 rows of B: us by it and by tiles of 128
-  //   32 rows: 4096 x 4096 6.1 and 10.6, 14336 x 4096 21 and 18, 8192 x 28672 54 and 39
-  //   64 rows: 1001 x 2056 6.9 and 11.1, 2000 x 8192 16.8 and 12.4, 32000 x 4096 74 and 30
-  const bool few = na <= 16 || (na <= kFewRows && double(na) * nb * nblocks * kMxBlock < 1e9);
+  // The kernel of few rows reads A again for every 16 rows of B and multiplies 16, 32 or 64 of A:
+  // us by it and by tiles of 128
+  //   4, 8 rows: 131072 x 8192 111 and 136, 32000 x 4096 20.5 and 19.7
+  //   16 rows: 14336 x 4096 12.8 and 14.2, 1001 x 65536 15.0 and 23.6, 32000 x 4096 22.6 and 20.4, 8192 x
+  //     28672 34 and 29
+  //   17, 32 rows: 4096 x 4096 5.4 and 9.7, 7000 x 4096 11.3 and 12.5, 14336 x 4096 18.2 and 14.3
+  //   64 rows: 1001 x 2056 6.9 and 11.1, 4096 x 4096 10.5 and 11.6, 14336 x 4096 37 and 17
+  const double work = double(na <= 16 ? 16 : na <= 32 ? 32 : 64) * double(nb) * double(nblocks * kMxBlock);
+  const bool few = na <= 8 || (na <= 16 && work < 1.8e9) || (na <= kFewRows && work < 1.1e9);
   if (few && nblocks >= 16) {
     const int64_t steps = (nblocks + 4 * kStep - 1) / (4 * kStep);
     p.b_tiles = int((nb + 15) / 16);
