@@ -120,12 +120,13 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 // place j ^ (r / 2 % 8) of the row's eight, so that the 16 bytes that neighbouring lanes
 // read, of neighbouring rows, spread over all banks. A lane's four exponents of a stage are
 // one register that the products pick their byte of.
-// 2048 x 32000 x 4096 take 175 to 187 us by box (2.9 to 3.1 PFLOP/s), 2048 x 8192 x 28672 293
-// (3.3), 512 x 14336 x 4096 24. Products alone, without loads, reach 6.7 PFLOP/s on random data
+// 2048 x 32000 x 4096 take 169 to 187 us by box (2.9 to 3.2 PFLOP/s), 2048 x 8192 x 28672 252
+// (3.8), 512 x 14336 x 4096 24. Products alone, without loads, reach 6.7 PFLOP/s on random data
 // and 5.2 with as many reads of LDS: power holds them, zeros take a quarter less. What else
 // bounds it are the waits at a stage's start. Exponents read by eight bytes of a row a lane took
 // 210 us, operands read right before their use 265. Tried and dropped: two workgroups a CU
-// with stages of 128 columns (216), the barrier before a stage's last step (registers spill).
+// with stages of 128 columns (216), the barrier before a stage's last step (registers spill),
+// four waves of 128 x 128, one a SIMD (324).
 constexpr int kBlocks = 8;   // of a stage
 
 template <int MT, int NT, int WM, int WN, bool SHORT, bool FULL>
