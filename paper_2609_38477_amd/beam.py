@@ -16,7 +16,7 @@ from dataclasses import dataclass
 
 from . import _check, _ptr, _stream
 from . import lib as _base_lib
-from .ops import _logits, _on, _rows, _same
+from .ops import _logits, _on, _rows, _same, _type
 
 SEEDQ_MAX_BEAMS = 32
 SEEDQ_MAX_BEAM_TOP = 32
@@ -94,18 +94,22 @@ def beam_select(logits, scores, top: int, finished=None, pad_token: int = 0, str
     A beam that is ``finished`` (bool or uint8 [batch, beams]) is continued by pad_token
     alone, at its own score."""
     L = _lib or lib()
-    t, device = _logits(logits, "logits")
-    nrows, vocab = logits.shape
-    if scores.dim() != 2 or not 1 <= scores.shape[1] <= SEEDQ_MAX_BEAMS:
-        raise ValueError(f"scores: [batch, 1 to {SEEDQ_MAX_BEAMS} beams] wanted, not {tuple(scores.shape)}")
-    batch, beams = scores.shape
+    t, device = _type(logits.dtype, "logits"), logits.get_device()
+    shape = logits.shape
+    if device < 0 or device != _current_device() or len(shape) != 2 or shape[1] < 1:
+        _logits(logits, "logits")   # names what is wrong
+    nrows, vocab = shape
+    shape = scores.shape
+    if len(shape) != 2 or not 1 <= shape[1] <= SEEDQ_MAX_BEAMS:
+        raise ValueError(f"scores: [batch, 1 to {SEEDQ_MAX_BEAMS} beams] wanted, not {tuple(shape)}")
+    batch, beams = shape
     if nrows != batch * beams:
         raise ValueError(f"logits: {batch * beams} rows wanted, not {nrows}")
     if not 1 <= top <= SEEDQ_MAX_BEAM_TOP:
         raise ValueError(f"top: 1 to {SEEDQ_MAX_BEAM_TOP} wanted, not {top}")
-    _same(scores, device, (batch, beams), torch.float32, "scores")
+    _same(scores, device, shape, torch.float32, "scores")
     if finished is not None:
-        _same(finished, device, (batch, beams), torch.bool if finished.dtype == torch.bool else torch.uint8,
+        _same(finished, device, shape, torch.bool if finished.dtype == torch.bool else torch.uint8,
               "finished")
         if pad_token < 0:
             raise ValueError(f"pad_token: not negative wanted, not {pad_token}")

@@ -138,7 +138,10 @@ def mx4_quantize(W, stream=None) -> Mx4Weights:
     t = _type(W.dtype, "W")
     if W.dim() != 2:
         raise ValueError(f"W: two dimensions wanted, not {W.dim()}")
-    return _with(stream, _quantize, L, W, t, _device(W, "W"))
+    device = W.get_device()
+    if device < 0 or device != _current_device():
+        _device(W, "W")   # names what is wrong
+    return _with(stream, _quantize, L, W, t, device)
 
 
 def _quantize(L, W, t, device):
