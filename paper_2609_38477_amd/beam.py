@@ -12,7 +12,10 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 from dataclasses import dataclass
+
+import numpy as np
 
 from . import _check, _ptr, _stream
 from . import lib as _base_lib
@@ -188,6 +191,69 @@ def _moved(shape, stride, to_stride, size: int):
     return src[0], dst[0], src[2], dst[2], src[1], src[3]
 
 
+class _Bytes:
+    """Bytes that numpy compares the addresses of and never reads."""
+
+    def __init__(self, start, shape, strides):
+        self.__array_interface__ = {"version": 3, "typestr": "|u1", "data": (start, False), "shape": shape,
+                                    "strides": strides}
+
+
+def _meet(intervals) -> bool:
+    """Whether one of the intervals (start, end, written) that is written meets another."""
+    end = end_written = -1   # of those that start before
+    for lo, hi, written in sorted(intervals):
+        if lo < (end if written else end_written):
+            return True
+        end = max(end, hi)
+        if written:
+            end_written = max(end_written, hi)
+    return False
+
+
+def _races(regions) -> bool:
+    """Whether one of the regions that is written shares a byte with another one. A region: (start,
+    stride of rows, rows, stride of pieces, pieces, bytes of a piece, written)."""
+    regions = sorted(regions)
+    ends = [at + (rows - 1) * row + (outer - 1) * step + inner
+            for at, row, rows, step, outer, inner, _ in regions]
+    first, end = 0, -1
+    for i, hi in enumerate(ends):   # those from first on lie in one stretch of memory
+        if regions[i][0] >= end:
+            if i - first > 1 and _races_near(regions[first:i], ends[first:i]):
+                return True
+            first = i
+        if hi > end:
+            end = hi
+    return len(ends) - first > 1 and _races_near(regions[first:], ends[first:])
+
+
+def _races_near(regions, ends) -> bool:
+    if not _meet([(r[0], end, r[6]) for r, end in zip(regions, ends)]):
+        return False
+    # Between each other's rows or pieces (the layers of one tensor): their places modulo a
+    # number that every stride is a multiple of.
+    by_row = math.gcd(*(row for _, row, rows, _, _, _, _ in regions if rows > 1))
+    by_piece = math.gcd(by_row, *(step for _, _, _, step, outer, _, _ in regions if outer > 1))
+    for by, whole in ((by_row, True), (by_piece, False)):
+        places = []
+        for at, _, _, step, outer, inner, written in regions:
+            n = inner + ((outer - 1) * step if whole else 0)
+            if by and n <= by:
+                at %= by
+                places += (at, at + n, written), (0, at + n - by, written)   # what goes on at the front
+        if len(places) == 2 * len(regions) and not _meet([p for p in places if p[0] < p[1]]):
+            return False
+    base = regions[0][0] - 1   # numpy takes no address 0
+    arrays = [(np.asarray(_Bytes(at - base, (rows, outer, inner), (row, step, 1))), written)
+              for at, row, rows, step, outer, inner, written in regions]
+    try:
+        return any(np.shares_memory(a, b, max_work=100000) for i, (a, v) in enumerate(arrays)
+                   for b, w in arrays[:i] if v or w)
+    except np.exceptions.TooHardError:
+        return True
+
+
 def beam_reorder(states, parents, out=None, stream=None):
     """The states of the beams that continue: row (i, j) of each result is row
     (i, parents[i, j]) of its tensor, zeros for a parent that is none of the sequence's.
@@ -195,9 +261,9 @@ def beam_reorder(states, parents, out=None, stream=None):
     states: a tensor or a list of tensors of any type on the GPU, [batch * beams, ...]
     each with the same number of rows; a row may be a part of a larger cache (a view).
     parents: int64 [batch, out_beams]. ``out``: tensors of the results' shapes and the
-    states' types that overlap nothing else of the call, or the states themselves, whose
-    rows are then moved in place (those that are their own parents stay untouched). Returns
-    a tensor or a list like states."""
+    states' types, or the states themselves, whose rows are then moved in place (those that
+    are their own parents stay untouched); one that shares memory with another result, another
+    state or the parents is refused. Returns a tensor or a list like states."""
     L = _lib or lib()
     single = isinstance(states, torch.Tensor)
     states = [states] if single else list(states)
@@ -264,11 +330,16 @@ def _reorder(L, states, parents, out, rows, batch, beams, out_beams, device):
             keep.append(s)
             at, moved = s.data_ptr(), _moved(shape, s.stride(), to, s.element_size())
         fields += (at, to_at, *moved)
-    if out is not None:
-        sources, targets = set(fields[::8]), fields[1::8]
-        if len(set(targets)) != len(targets) or any(
-                to != at and to in sources for at, to in zip(fields[::8], targets)):
-            raise ValueError("out: tensors that are no other result's and no other state wanted")
+    if out is not None and fields:
+        regions = [(parents.data_ptr(), 0, 1, 0, 1, 8 * out_rows, False)]
+        for i in range(0, len(fields), 8):
+            at, to_at, row, to_row, step, to_step, outer, inner = fields[i:i + 8]
+            regions.append((to_at, to_row, out_rows, to_step, outer, inner, True))
+            if at != to_at:
+                regions.append((at, row, rows, step, outer, inner, False))
+        if _races(regions):
+            raise ValueError("out: tensors that share no memory with another result, another state or the "
+                             "parents wanted")
     if fields:
         array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
         _check(L.seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,
