@@ -27,7 +27,8 @@ extern "C" {
  * sequences, which have `beams` (1 .. SEEDQ_MAX_BEAMS) beams each. Beam b of a
  * sequence, whose score so far is s_b, offers every token v of its row x of logits with
  *     total = s_b + (x_v - log sum e^x),
- * the sum in fp32 or wider over blocks and fp64 over them, the rest in fp64. A finished beam
+ * exponentials and sums of two of them in fp32, the rest in fp64: the log of the sum errs by less
+ * than 1.75e-7, and the total becomes fp32 once. A finished beam
  * offers pad_token alone, with total s_b. Continuations come by falling total, equal
  * totals by rising beam, equal ones of a beam by falling logit and rising token.
  *   d_logits: type [batch beams][vocab], row stride ld >= vocab; what lies between

@@ -2,6 +2,7 @@
 // beams moved to those that continue them.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "seedq_beam_internal.h"
 #include "seedq_top.h"
@@ -9,8 +10,8 @@
 namespace seedq {
 namespace {
 
-constexpr float kLog2E = 1.44269504088896340736f;
-constexpr float kFar = -1e30f;      // stands in for x - m = -inf: its e^ is 0
+constexpr double kLog2EExact = 1.44269504088896340736, kLn2 = 0.693147180559945309417;
+constexpr float kLog2E = float(kLog2EExact), kLog2E16 = 0x1.7154p0f, kLn2High = float(kLn2), kLn2Low = float(kLn2 - double(kLn2High));
 constexpr int kUnroll = 4;          // vectors in flight a thread
 constexpr int kMaxSegs = 16;
 constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
@@ -18,15 +19,31 @@ static_assert(SEEDQ_MAX_BEAM_TOP <= kMaxTop, "the selection of a row");
 
 // ---------------------------------------------------------------- selection
 //
-// total(b, v) = s_b + (x_bv - m_b) - log S_b with m_b the largest logit of beam b and S_b =
-// sum e^(x - m_b). Within a beam the order is that of the logits, so no more than the `top`
-// largest of each row can be among a sequence's: the first kernel goes over the logits once
-// and leaves of every row, or segment of one, m, S and the keys of its largest elements,
-// the second ranks what the beams of a sequence offer. Totals of different beams may lie
-// next to each other, so each vector quartet's sum joins S in fp64.
+// total(b, v) = s_b + (x_bv - log sum e^x_b). Within a beam the order is that of the logits, so no
+// more than the `top` largest of each row can be among a sequence's: the first kernel goes over
+// the logits once and leaves of every row, or segment of one, its sum of exponentials and the
+// keys of its largest elements, the second ranks what the beams of a sequence offer.
+//
+// Totals of different beams may lie next to each other, and where many tokens lie as far below
+// the largest as each other, what one term errs by the sum errs by. So a term is rounded in the
+// exponential alone, by 8.5e-8 of itself at the most (the instruction over all arguments); what
+// its argument was rounded by is added to the sum. Pairs (6e-8) are joined in fp64. The sum errs
+// by less than 1.75e-7 of itself, 2.8e-8 of them the square of a bfloat16 argument's rest, next to
+// +-48. Exponentials of fp32 differences and sums of 32 of them took 6.4e-7, for 131072 equal
+// logits 11 below the largest.
+//
 // Memory bounds the first: 512 rows of 131072 bf16 logits take 29 us (4.6 TB/s); 4 rows of
 // 32003 fp32 7, latency. The second takes 7 us for 64 sequences of 8 beams, 5.5 for one, its
 // way from load to load (13 and 9 where it read keys when it needed them).
+
+// A sum stands for e^at times as much, at being 0 for a largest element of less than 48 either way,
+// so that its terms are powers of the logits themselves, and else that element: fp32 then holds the
+// differences to all that count.
+__device__ __forceinline__ float scale_of(float m) { return fabsf(m) < 48.f ? 0.f : m; }
+__device__ __forceinline__ double rescaled(double S, float from, float to) {
+  if (from == to || S == 0.0) return S;
+  return S * exp2((double(from) - double(to)) * kLog2EExact);
+}
 
 struct Partial {
   double S;
@@ -53,16 +70,32 @@ beam_rows_kernel(BeamArgs a, uint32_t segs, uint32_t seg_vectors, Partial* __res
   const uint32_t begin = std::min(seg * seg_vectors, row.vectors);
   const uint32_t end = std::min(begin + seg_vectors, row.vectors);
   float m = -FLT_MAX, best = -kInf;
+  float scale = m;
   double S = 0.0;
   uint32_t base = 0;
   const auto raise = [&](float to) {
     if (to > m) {
-      S *= double(__builtin_amdgcn_exp2f(fmaxf(m - to, kFar) * kLog2E));
       m = to;
+      S = rescaled(S, scale, scale_of(m));
+      scale = scale_of(m);
     }
   };
-  const auto term = [&](float x) {   // a NaN stays one: m is infinite only without a distribution
-    return __builtin_amdgcn_exp2f(__builtin_elementwise_maximum(x - m, kFar) * kLog2E);
+  // The terms of all vectors. e^c = 2^p e^(c - p log 2), of which the second factor less 1, times the
+  // first, is added up apart. p is c log2 e, and of a bfloat16 the product with the first 16 bits of
+  // log2 e, which is exact. A NaN stays one and +inf becomes one; -inf is 0.
+  const auto add = [&](const float (&f)[N], float& rest, auto whole) {
+    constexpr bool kScaled = !decltype(whole)::value, kExact = !kScaled && std::is_same_v<T, BF16>;
+    const auto term = [&](float x) {
+      const float c = __builtin_elementwise_maximum(kScaled ? x - scale : x, -104.f);
+      const float p = c * (kExact ? kLog2E16 : kLog2E), e = __builtin_amdgcn_exp2f(p);
+      rest = fmaf(e, kExact ? c : fmaf(p, -kLn2Low, fmaf(p, -kLn2High, c)), rest);
+      return e;
+    };
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      const float a = term(f[k]);
+      S += double(a + term(f[k + 1]));
+    }
   };
   const auto note = [&](float l, uint32_t at) {
     if (l > best) {
@@ -78,7 +111,7 @@ beam_rows_kernel(BeamArgs a, uint32_t segs, uint32_t seg_vectors, Partial* __res
       v[u] = minus_infinity<T>();   // adds nothing
       if (i + u * NT + tid < end) v[u] = row.load(i + u * NT + tid);
     }
-    float f[kUnroll][N], top = -kInf, sum = 0.f;
+    float f[kUnroll][N], top = -kInf;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       widen<T>(v[u], f[u]);
@@ -87,19 +120,22 @@ beam_rows_kernel(BeamArgs a, uint32_t segs, uint32_t seg_vectors, Partial* __res
       top = fmaxf(top, l);
     }
     raise(top);
+    const auto all = [&](auto whole) {
+      float rest = 0.f;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (i + u * NT < end)
-#pragma unroll
-        for (int k = 0; k < N; ++k) sum += term(f[u][k]);
-    S += double(sum);
+      for (int u = 0; u < kUnroll; ++u)
+        if (i + u * NT < end) add(f[u], rest, whole);
+      S += double(rest) * (decltype(whole)::value && std::is_same_v<T, BF16> ? 1.0 - double(kLog2E16) * kLn2 : 1.0);
+    };
+    if (__any(scale != 0.f)) all(std::false_type{});
+    else all(std::true_type{});
   }
   const uint32_t after = row.vectors * N;
   const bool has_tail = seg == segs - 1 && tid < row.tail;   // elements after the last vector
   if (has_tail) {
     const float x = T::widen(row.x[after + tid]);
     raise(x);
-    S += double(term(x));
+    S += exp(double(x) - double(scale));
     note(x, after + tid);
   }
   const Key mine = best > -kInf ? order_key(best, base) : 0;
@@ -110,7 +146,7 @@ beam_rows_kernel(BeamArgs a, uint32_t segs, uint32_t seg_vectors, Partial* __res
   __syncthreads();
   most = sf[0];
   for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sf[w]);
-  S *= double(__builtin_amdgcn_exp2f(fmaxf(m - most, kFar) * kLog2E));
+  S = rescaled(S, scale, scale_of(most));
   S = lanes_reduce(S, [](double p, double q) { return p + q; });
   if (lane == 0) sd[wave] = S;
   top_note<NT>(chosen, mine);
@@ -198,10 +234,10 @@ beam_join_kernel(BeamArgs a, int segs, const Partial* __restrict__ partial,
       const Partial* p = part + tid * segs;
       float m = p[0].m;
       for (int g = 1; g < segs; ++g) m = fmaxf(m, p[g].m);
+      const float scale = scale_of(m);
       double S = 0.0;
-      for (int g = 0; g < segs; ++g)
-        S += double(__builtin_amdgcn_exp2f(fmaxf(p[g].m - m, kFar) * kLog2E)) * p[g].S;
-      most[tid] = m;
+      for (int g = 0; g < segs; ++g) S += rescaled(p[g].S, scale_of(p[g].m), scale);
+      most[tid] = double(scale);
       log_s[tid] = log(S);
       k = S > 0.0 ? kTokens : S == 0.0 ? kNone : kBad;
     }
