@@ -344,4 +344,6 @@ def _reorder(L, states, parents, out, rows, batch, beams, out_beams, device):
         array = (ctypes.c_int64 * len(fields))(*fields)   # BeamStates
         _check(L.seedq_beam_reorder(array, len(fields) // 8, parents.data_ptr(), batch, beams,
                                     out_beams, _handle(device)), "seedq_beam_reorder")
+    if out is not None:
+        torch.autograd.graph.increment_version(results)   # written, as autograd counts it
     return results

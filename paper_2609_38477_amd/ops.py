@@ -346,7 +346,8 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None
             _same(v, device, (nrows,), torch.float32, name)
     with _on(stream):
         x, ld = _rows(logits)
-        if out is None:
+        given = out is not None
+        if not given:
             out, ldg = x.new_empty((nrows, vocab)), vocab
         elif out.dtype != x.dtype or out.shape != x.shape or out.get_device() != device \
                 or (vocab > 1 and out.stride(1) != 1) or (nrows > 1 and out.stride(0) < vocab):
@@ -358,4 +359,6 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None
                                                    _ptr(grad_entropy), out.data_ptr(), ldg,
                                                    _handle(device)),
                "seedq_token_logprobs_backward")
+    if given:
+        torch.autograd.graph.increment_version(out)   # written, as autograd counts it
     return out
