@@ -98,7 +98,8 @@ def beam_search(step, states, tokens, beams: int, length: int, eos: int = -1, pa
 
 def continuations(head, embed, h, beams: int = 4, length: int = 8):
     """Beam search on a head by itself: head(h [n, d]) gives logits, and the state after a
-    token is h plus the token's row of embed [vocab, d], brought back to h's size."""
+    token is h plus the token's row of embed [vocab, d] (nothing of a row of zeros), brought back
+    to h's size."""
     import torch
     size = h.square().mean(1, keepdim=True).sqrt()
     first = True
@@ -108,7 +109,7 @@ def continuations(head, embed, h, beams: int = 4, length: int = 8):
         h, size = states
         if not first:   # h stands after the tokens that were there
             row = embed[tokens]
-            h = h + row * (size / row.square().mean(1, keepdim=True).sqrt())
+            h = h + row * (size / row.square().mean(1, keepdim=True).sqrt().clamp(min=1e-20))
             h = h * (size / h.square().mean(1, keepdim=True).sqrt().clamp(min=1e-20))
         first = False
         return head(h), [h, size]
