@@ -93,6 +93,9 @@ def beam_search(step, states, tokens, beams: int, length: int, eos: int = -1, pa
         history.masked_fill_((r.token.view(-1) < 0).unsqueeze(1), -1)
         finished |= r.token == eos
         scores, tokens = r.score, r.token.view(-1).clamp(min=0)
+    if length == 0:   # the one continuation of no tokens
+        scores = torch.nn.functional.pad(scores, (0, beams - 1), value=-math.inf)
+        history = history.new_empty((batch * beams, 0))
     return history.view(batch, beams, length), scores
 
 
