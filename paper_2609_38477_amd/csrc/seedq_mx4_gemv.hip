@@ -265,8 +265,11 @@ hipError_t launch_few(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx, 
     constexpr int NV = decltype(nv)::value;
     // Two rows a wave share what is read of x: 32000 x 4096 15.0 us (one row 17.0), and two
     // vectors 18.3 (20.1); 14336 x 4096 and two 10.8 (9.7), 1001 x 2056 and three of fp32 6.2 (5.3).
-    const bool two = q.nrows >= 16384;
-    two ? go(few_kernel<X, NV, 2>, NV, 2, v) : go(few_kernel<X, NV, 1>, NV, 1, v);
+    // Three and four vectors come with up to 8192 rows only, or with rows so long that there are
+    // fewer than 4096.
+    if constexpr (NV <= 2)
+      if (q.nrows >= 16384) return go(few_kernel<X, NV, 2>, NV, 2, v);
+    go(few_kernel<X, NV, 1>, NV, 1, v);
   };
   for (int64_t v = 0; v < nvec; v += 4) {
     const int64_t n = nvec - v;
