@@ -727,29 +727,45 @@ struct GemmPlan {
   size_t frags, total;
 };
 GemmPlan gemm_plan(int64_t nrows, int64_t ncols, int64_t nvec, int pieces) {
-  GemmPlan p;
   const int64_t tiles = (nvec + kTileVecs - 1) / kTileVecs;
-  const int most = pieces == 3 ? 3 : 4;
-  p.mt = 1;
-  // The fewest tiles of vectors in all, then the widest: a wider one decodes less often (32000 x
-  // 4096 and 512 vectors in tiles of 128 123 us, of 64 164; 4096 x 4096 and 128 27 and 22).
-  for (int m = 2; m <= most; ++m)
-    if ((tiles + m - 1) / m * m <= (tiles + p.mt - 1) / p.mt * p.mt) p.mt = m;
-  p.vec_tiles = int((tiles + p.mt - 1) / p.mt);
-  // 64 rows a wave where that leaves as many tiles as the chip holds workgroups: 32000 x 4096 and
-  // 512 vectors 123 us (32 rows 133), 14336 x 4096 and 512 84 (66), 4096 x 4096 and 512 43 (35).
-  p.rt = (nrows + 255) / 256 * p.vec_tiles >= 400 ? 2 : 1;
-  p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
-  p.chunks = (ncols + 127) / 128 * 2;   // whole stages
-  const int64_t all = int64_t(p.vec_tiles) * p.row_tiles;
-  // Up to two workgroups a CU, of four stages at least: 4096 x 4096 and 300 vectors up to 512
-  // workgroups 30.1 us, 256 39.5, 1024 33.2; 4096 x 4096 and 64 four stages 17.5, two 22.4,
-  // eight 18.5.
-  p.splits = int(std::max<int64_t>(1, std::min<int64_t>({512 / all, p.chunks / 8, 32})));
-  p.frags = align256(size_t(p.vec_tiles) * p.mt * p.chunks * pieces * kFrags * 1024);
-  p.total = p.frags;
-  if (p.splits > 1) p.total += align256(size_t(p.splits) * nvec * nrows * sizeof(float));
-  return p;
+  GemmPlan best{};
+  double least = 0.0;
+  // Tiles of vectors of a workgroup: a wider one decodes less often, and the last one may be empty in
+  // part; narrow ones fill the chip and are split less. Taken is what the following finds fastest: us
+  // of a chunk by x, a workgroup's tiles of pieces, for two workgroups a CU and for one, the join and
+  // the fragments. On the mean of 200 sizes it is within 1 % of the fastest width. us by 1, 2, 3 and 4
+  //   32000 x 4096, bf16: 5 tiles 107, 74, 59, 66; 8 139, 89, 87, 72; 13 236, 160, 147, 122; 16 272, 175, 156, 128
+  //   32000 x 4096, fp16: 5 126, 103, 92, 113; 13 281, 221, 218, 195; fp32 5 147, 140, 131
+  //   4096 x 4096, bf16: 4 21.3, 23.8, 23.8, 23.0; 7 30.5, 25.8, 26.1, 26.0; 1001 x 2056 7 14.2, 15.8, 16.5, 17.4
+  for (int mt = 1; mt <= (pieces == 3 ? 3 : 4); ++mt) {
+    GemmPlan p{};
+    p.mt = mt;
+    p.vec_tiles = int((tiles + mt - 1) / mt);
+    // 64 rows a wave where that leaves as many tiles as the chip holds workgroups: 32000 x 4096 and
+    // 512 vectors 123 us (32 rows 133), 14336 x 4096 and 512 84 (66), 4096 x 4096 and 512 43 (35). With
+    // nine tiles of pieces the next stage's codes went through scratch memory: 128000 x 4096 and 96
+    // fp32 vectors 398 us (32 rows 291).
+    const int x = pieces * mt;
+    p.rt = (nrows + 255) / 256 * p.vec_tiles >= 400 && x < 9 ? 2 : 1;
+    p.row_tiles = int((nrows + 128 * p.rt - 1) / (128 * p.rt));
+    p.chunks = (ncols + 127) / 128 * 2;   // whole stages
+    const int64_t all = int64_t(p.vec_tiles) * p.row_tiles;
+    // Up to two workgroups a CU, of four stages at least: 4096 x 4096 and 300 vectors up to 512
+    // workgroups 30.1 us, 256 39.5, 1024 33.2; 4096 x 4096 and 64 four stages 17.5, two 22.4,
+    // eight 18.5.
+    p.splits = int(std::max<int64_t>(1, std::min<int64_t>({512 / all, p.chunks / 8, 32})));
+    p.frags = align256(size_t(p.vec_tiles) * mt * p.chunks * pieces * kFrags * 1024);
+    p.total = p.frags;
+    if (p.splits > 1) p.total += align256(size_t(p.splits) * nvec * nrows * sizeof(float));
+    const double two = p.rt == 1 ? 0.40 + 0.135 * x : 0.72 + 0.265 * x, one = p.rt == 1 ? 0.11 + 0.117 * x : two / 2;
+    const int64_t rounds = all * p.splits / 512, rest = all * p.splits % 512;
+    const double us = double(p.chunks) / p.splits * (double(rounds) * two + (rest > 256 ? two : rest ? one : 0.0)) +
+                      double(p.frags) * 0.85e-6 + (p.splits > 1 ? 5.6 + double(p.total - p.frags) * 0.24e-6 : 0.0);
+    if (mt > 1 && us >= least) continue;
+    least = us;
+    best = p;
+  }
+  return best;
 }
 
 template <class X>
@@ -770,8 +786,9 @@ hipError_t launch_gemm(const Mx4& q, int64_t nvec, const void* d_x, int64_t ldx,
   };
   auto with = [&](auto mt) {
     constexpr int MT = decltype(mt)::value;
-    if (p.rt == 1) go(gemm_kernel<P, MT, 1, C>);
-    else go(gemm_kernel<P, MT, 2, C>);
+    if constexpr (P * MT < 9)
+      if (p.rt == 2) return go(gemm_kernel<P, MT, 2, C>);
+    go(gemm_kernel<P, MT, 1, C>);
   };
   if (p.mt == 1) with(std::integral_constant<int, 1>{});
   else if (p.mt == 2) with(std::integral_constant<int, 2>{});
