@@ -32,8 +32,8 @@ static_assert(SEEDQ_MAX_BEAM_TOP <= kMaxTop, "the selection of a row");
 // +-48. Exponentials of fp32 differences and sums of 32 of them took 6.4e-7, for 131072 equal
 // logits 11 below the largest.
 //
-// Memory bounds the first: 512 rows of 131072 bf16 logits take 29 us (4.6 TB/s); 4 rows of
-// 32003 fp32 7, latency. The second takes 7 us for 64 sequences of 8 beams, 5.5 for one, its
+// Memory bounds the first: 512 rows of 131072 bf16 logits take 29 to 31 us (4.3 to 4.6 TB/s); 4 rows
+// of 32003 fp32 7, latency. The second takes 7 us for 64 sequences of 8 beams, 6 for one, its
 // way from load to load (13 and 9 where it read keys when it needed them).
 
 // A sum stands for e^at times as much, at being 0 for a largest element of less than 48 either way,
@@ -355,8 +355,10 @@ size_t rows_bytes(int64_t rows, int64_t vocab, int top) {
 // Units of 16 bytes of the pieces' lengths, the last of a piece shorter. A thread takes the
 // same unit of all rows of a sequence: it reads those of the parents, then writes, so that a
 // tensor can be its own destination, every parent's unit comes from memory once, and rows
-// that stay are left alone. Memory bounds it: 32 tensors of 16 beams, 2.65 GB read and
-// written, take 500 to 580 us (4.5 to 5.3 TB/s), four small ones 7.
+// that stay are left alone. Memory bounds it: 32 tensors of four sequences of four beams, 2.65 GB
+// read and written, take 540 to 620 us by box and parents (4.1 to 4.9 TB/s), four small ones 7. Of
+// one sequence of 16 or 32 beams 3.9 and 4.4 TB/s, of 5 and 8, whose kernel holds 238 registers a
+// lane, 2.4 and 2.9; the same in place, less the rows that stay.
 struct State {
   const char* src;
   char* dst;

@@ -26,9 +26,10 @@ __device__ __forceinline__ intx8 fp4_operand(uint32x4 c) {
 // 16 AT rows of A against 16 rows of B a workgroup. The waves divide the columns in steps of
 // 512, whose codes and exponents a lane reads straight into registers, the next step's
 // during the products; their sums meet in LDS in order. A's rows are the same for all
-// workgroups and come from the caches. 4 x 4096 x 4096 take 4.2 us, some 2 of them an empty
+// workgroups and come from the caches. 4 x 4096 x 4096 take 4.3 us, some 2 of them an empty
 // launch, 4 x 8192 x 28672 29 (4.3 TB/s), bound by memory; 16 x 8192 x 28672 37, bound by the
-// loads of A.
+// loads of A, where tiles take 33. With 64 rows of A (10.5 us at 4096 x 4096) 16 registers lie in
+// scratch memory.
 constexpr int kStep = 4;        // products of a step
 constexpr int kFewWaves = 8;
 
@@ -120,8 +121,9 @@ few_kernel(Mx4 a, Mx4 b, int splits, void* __restrict__ y, int ytype, int64_t ld
 // place j ^ (r / 2 % 8) of the row's eight, so that the 16 bytes that neighbouring lanes
 // read, of neighbouring rows, spread over all banks. A lane's four exponents of a stage are
 // one register that the products pick their byte of.
-// 2048 x 32000 x 4096 take 169 to 187 us by box (2.9 to 3.2 PFLOP/s), 2048 x 8192 x 28672 252
-// (3.8), 512 x 14336 x 4096 24. Products alone, without loads, reach 6.7 PFLOP/s on random data
+// 2048 x 32000 x 4096 take 169 to 188 us by box (2.9 to 3.2 PFLOP/s; the matrix core is busy for 41 %
+// of the time), 2048 x 8192 x 28672 250 (3.8), 512 x 14336 x 4096 24, and 29 with codes that come from
+// memory. Products alone, without loads, reach 6.7 PFLOP/s on random data
 // and 5.2 with as many reads of LDS: power holds them, zeros take a quarter less. What else
 // bounds it are the waits at a stage's start. Exponents read by eight bytes of a row a lane took
 // 210 us, operands read right before their use 265. Tried and dropped: two workgroups a CU
@@ -301,12 +303,14 @@ struct Plan {
 Plan plan(int64_t na, int64_t nb, int64_t nblocks) {
   Plan p{};
   // The kernel of few rows reads A again for every 16 rows of B and multiplies 16, 32 or 64 of A:
-  // us by it and by tiles of 128
-  //   4, 8 rows: 131072 x 8192 111 and 136, 32000 x 4096 20.5 and 19.7
-  //   16 rows: 14336 x 4096 12.8 and 14.2, 1001 x 65536 15.0 and 23.6, 32000 x 4096 22.6 and 20.4, 8192 x
-  //     28672 34 and 29
-  //   17, 32 rows: 4096 x 4096 5.4 and 9.7, 7000 x 4096 11.3 and 12.5, 14336 x 4096 18.2 and 14.3
-  //   64 rows: 1001 x 2056 6.9 and 11.1, 4096 x 4096 10.5 and 11.6, 14336 x 4096 37 and 17
+  // us by it and by tiles of 128, the codes of large matrices from memory
+  //   4 rows: 131072 x 8192 110 and 135, 32000 x 4096 20.8 and 22.2, 8192 x 28672 28.9 and 32.0
+  //   8 rows: 131072 x 8192 123 and 136, 32000 x 4096 22.1 and 22.5, 8192 x 28672 32.1 and 32.1
+  //   16 rows: 14336 x 4096 13.4 and 15.7, 1001 x 65536 16.4 and 28.7, 32000 x 4096 23.9 and 23.3, 8192 x
+  //     28672 37.2 and 32.8
+  //   17 rows: 4096 x 4096 5.3 and 9.6; 32: 4096 x 4096 6.1 and 10.6, 7000 x 4096 10.8 and 11.4, 14336 x
+  //     4096 22.7 and 16.9
+  //   64 rows: 1001 x 2056 7.0 and 11.1, 4096 x 4096 10.5 and 11.6, 14336 x 4096 38.5 and 19.4
   const double work = double(na <= 16 ? 16 : na <= 32 ? 32 : 64) * double(nb) * double(nblocks * kMxBlock);
   const bool few = na <= 8 || (na <= 16 && work < 1.8e9) || (na <= kFewRows && work < 1.1e9);
   if (few && nblocks >= 16) {
